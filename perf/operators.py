@@ -346,8 +346,9 @@ def _plain_scored(st):
 
 
 def _plain_draw(logits, u, temperature, top_k, top_p, min_p):
-    """Tokens of rows of logits, and the logarithms of their probabilities.  In
-    64 bits: a token is a comparison of sums over the whole vocabulary."""
+    """Tokens of rows of logits (the first in order of falling probability whose
+    cumulative share passes u), and the logarithms of their probabilities.  In 64
+    bits: a token is a comparison of sums over the whole vocabulary."""
     x = logits.double() + 0.0
     V = x.shape[1]
     d = (x.amax(1, keepdim=True) - x) / temperature[:, None].double()
@@ -362,11 +363,10 @@ def _plain_draw(logits, u, temperature, top_k, top_p, min_p):
         w = torch.where(keep, w, 0.0)
     if min_p is not None:
         w = torch.where(w >= min_p[:, None].double(), w, 0.0)
-    w = torch.zeros_like(w).scatter_(1, order.indices, w)
     z = w.cumsum(1)
-    token = (z <= u[:, None].double() * z[:, -1:]).sum(1)
-    p = w.gather(1, token[:, None]).squeeze(1) / z[:, -1]
-    return token.int(), torch.log(p).float()
+    at = (z <= u[:, None].double() * z[:, -1:]).sum(1, keepdim=True)
+    p = w.gather(1, at) / z[:, -1:]
+    return order.indices.gather(1, at).squeeze(1).int(), torch.log(p).squeeze(1).float()
 
 
 def _plain_sample(st):
@@ -419,12 +419,13 @@ def _own_run(st):
                                      softcap=st["cap"], slopes=st["slopes"], window=st["window"],
                                      starts=st["starts"], draft_mask=st["mask"], block_table=st["table"],
                                      out=st["out"], lse=st["lse"], workspace=st["ws"])
-    if "ws" not in st:
-        st["ws"] = sm.alloc_sample_workspace(st["logits"])
-    params = dict(temperature=st["temperature"], top_k=st["top_k"], top_p=st["top_p"], min_p=st["min_p"],
-                  out=st["out"], workspace=st["ws"])
+    params = {n: st[n] for n in ("temperature", "top_k", "top_p", "min_p", "out")}
     if op == "sample":
         return sm.sample(st["logits"], st["u"], **params)
+    if "ws" not in st:
+        code = {torch.float32: sm.binding.SPECMOE_F32, torch.bfloat16: sm.binding.SPECMOE_BF16}[st["logits"].dtype]
+        st["ws"] = sm.alloc_accept_workspace(sm.accept_desc(*st["logits"].shape, code), st["logits"].device)
+    params["workspace"] = st["ws"]
     if op == "accept":
         return sm.accept_sample(st["logits"], st["tokens"], st["ctx"], st["chunk"], st["u"], **params)
     return sm.accept_sample_tree(st["logits"], st["tokens"], st["mask"], st["ctx"], st["chunk"], st["u"], **params)
@@ -526,8 +527,8 @@ def _exact_scored(st):
 
 
 def _exact_draw(x, u, temperature, k, p, min_p):
-    """One row, on the host: the kept tokens by sorting, the token by walking
-    through their masses in token order."""
+    """One row, on the host: the most probable tokens first, cut down by each
+    setting in turn."""
     order = np.lexsort((np.arange(x.size), -x))
     w = np.exp((x - x[order[0]]) / temperature)[order]
     n = k if k and k > 0 else x.size
@@ -538,10 +539,9 @@ def _exact_draw(x, u, temperature, k, p, min_p):
     if min_p is not None:
         n = int((w >= min_p).sum())
         w, order = w[:n], order[:n]
-    by_token = np.argsort(order)
-    cum = np.cumsum(w[by_token])
+    cum = np.cumsum(w)
     n = int(np.searchsorted(cum, u * cum[-1], side="right"))
-    return int(order[by_token[n]]), math.log(w[by_token[n]] / cum[-1])
+    return int(order[n]), math.log(w[n] / cum[-1])
 
 
 def _exact_sample(st):
