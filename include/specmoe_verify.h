@@ -67,9 +67,14 @@ enum {
   SPECMOE_ERR_PAGES = -14,        /* paged cache: page_size not a power of two in
                                      [8, 65536], pages_per_seq or num_pages < 1, or
                                      S_max != page_size * pages_per_seq               */
-  SPECMOE_ERR_HANDOFF = -15       /* (specmoe_verify_attn_status) a kernel's wait for
+  SPECMOE_ERR_HANDOFF = -15,      /* (specmoe_verify_attn_status) a kernel's wait for
                                      another wave of its workgroup gave up: the
                                      results of that call are unspecified            */
+  SPECMOE_ERR_ROPE = -16,         /* (specmoe_append_kv) rot_dim is not a multiple of 16
+                                     in [0, D], rope_style is not a specmoe_rope_style,
+                                     or norm_eps is negative or not finite           */
+  SPECMOE_ERR_SCORE = -17         /* (specmoe_verify_attn_scored) softcap or window is
+                                     negative, or softcap is not finite              */
 };
 
 /* desc->flags bits. */

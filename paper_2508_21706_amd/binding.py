@@ -25,7 +25,9 @@ STATUS = {
     -4: "SPECMOE_ERR_HEAD_DIM", -5: "SPECMOE_ERR_DTYPE", -6: "SPECMOE_ERR_ROWS", -7: "SPECMOE_ERR_GRID",
     -8: "SPECMOE_ERR_WORKSPACE", -9: "SPECMOE_ERR_ALIGN", -10: "SPECMOE_ERR_SCALE", -11: "SPECMOE_ERR_LAUNCH",
     -12: "SPECMOE_ERR_FLAGS", -13: "SPECMOE_ERR_MASK", -14: "SPECMOE_ERR_PAGES", -15: "SPECMOE_ERR_HANDOFF",
+    -16: "SPECMOE_ERR_ROPE", -17: "SPECMOE_ERR_SCORE",
 }
+ROPE_STYLES = {"halves": 0, "pairs": 1}   # specmoe_rope_style
 SPECMOE_FLAG_NO_WAIT = 1
 
 
@@ -51,6 +53,28 @@ class AcceptDesc(ctypes.Structure):
 class PagedKV(ctypes.Structure):
     """Mirror of ``specmoe_paged_kv``."""
     _fields_ = [("page_size", ctypes.c_int32), ("pages_per_seq", ctypes.c_int32), ("num_pages", ctypes.c_int32)]
+
+
+class AppendDesc(ctypes.Structure):
+    """Mirror of ``specmoe_append_desc``."""
+    _fields_ = [
+        ("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("C_max", ctypes.c_int32), ("S_max", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+        ("rope_style", ctypes.c_int32), ("norm_eps", ctypes.c_float),
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+    ]
+
+
+class SampleDesc(ctypes.Structure):
+    """Mirror of ``specmoe_sample_desc``."""
+    _fields_ = [("N", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_int32),
+                ("stride", ctypes.c_int64)]
+
+
+class Sampling(ctypes.Structure):
+    """Mirror of ``specmoe_sampling``."""
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p),
+                ("min_p", ctypes.c_void_p)]
 
 
 class SpecMoEError(RuntimeError):
@@ -105,6 +129,17 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.specmoe_accept_workspace_init.restype = ctypes.c_int
     lib.specmoe_accept_workspace_init.argtypes = [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p,
                                                   ctypes.POINTER(AcceptDesc)]
+    lib.specmoe_append_kv.restype = ctypes.c_int
+    lib.specmoe_append_kv.argtypes = [ctypes.c_void_p] * 14 + [ctypes.POINTER(AppendDesc), ctypes.POINTER(PagedKV)]
+    lib.specmoe_sample.restype = ctypes.c_int
+    lib.specmoe_sample.argtypes = [ctypes.c_void_p] * 2 + [ctypes.POINTER(Sampling)] + [ctypes.c_void_p] * 3 + [
+        ctypes.POINTER(SampleDesc)]
+    lib.specmoe_accept_sample.restype = ctypes.c_int
+    lib.specmoe_accept_sample.argtypes = [ctypes.c_void_p] * 5 + [ctypes.POINTER(Sampling)] + [ctypes.c_void_p] * 6 + [
+        ctypes.POINTER(AcceptDesc)]
+    lib.specmoe_accept_sample_tree.restype = ctypes.c_int
+    lib.specmoe_accept_sample_tree.argtypes = [ctypes.c_void_p] * 6 + [ctypes.POINTER(Sampling)] + [
+        ctypes.c_void_p] * 7 + [ctypes.POINTER(AcceptDesc)]
     lib.specmoe_status_str.restype = ctypes.c_char_p
     lib.specmoe_status_str.argtypes = [ctypes.c_int]
     if path is None:
@@ -488,3 +523,224 @@ def accept_greedy(logits: torch.Tensor, tokens: torch.Tensor, ctx_lens: torch.Te
     if st != 0:
         raise SpecMoEError(st, status_str(st))
     return out
+
+
+# ------------------------------------------------------------- chunk append
+
+def _check_on(t: torch.Tensor, name: str, shape, dtype, device):
+    _check(t, name, shape, dtype)
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+
+
+def _launch(t: torch.Tensor, call, *args):
+    """A library call with ``t``'s GPU current; raises on an error status."""
+    if t.get_device() == torch.cuda.current_device():
+        st = call(*args)
+    else:
+        with torch.cuda.device(t.device):
+            st = call(*args)
+    if st != 0:
+        raise SpecMoEError(st, status_str(st))
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _token_stride(t: torch.Tensor, name: str, shape, dtype, device) -> int:
+    """Elements from one token's row of ``t`` [B, C_max, H, D] to the next's;
+    a row's heads lie side by side."""
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or t.device != device:
+        _check_on(t, name, shape, dtype, device)
+    B, C, H, D = shape
+    if t.is_contiguous():
+        return H * D
+    sb, sc, sh, sd = t.stride()
+    stride = sc if C > 1 else sb if B > 1 else H * D
+    if (D > 1 and sd != 1) or (H > 1 and sh != D) or (B > 1 and C > 1 and sb != C * sc):
+        raise ValueError(f"{name} must be rows of side-by-side heads at one distance from token to token")
+    return stride
+
+
+def append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor,
+              v_cache: torch.Tensor, ctx_lens: torch.Tensor, chunk_lens: torch.Tensor,
+              inv_freq: Optional[torch.Tensor] = None, rope: str = "halves",
+              q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+              draft_mask: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None,
+              q_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Norm and rotate a chunk's queries and keys and append its keys and
+    values to the cache; see ``specmoe_append_kv`` in
+    ``include/specmoe_append.h``.  The step before ``verify_attn``.
+
+    q [B, C_max, Hq, D], k / v [B, C_max, Hkv, D] (bf16, f16 or f32), possibly
+    views of one packed projection; k_cache / v_cache [B, Hkv, S_max, D], or
+    with ``block_table`` the pages of ``verify_attn_paged``.  ``inv_freq``
+    float64 [rot_dim / 2] (None: no rotation); ``rope`` "halves" or "pairs";
+    ``q_weight`` / ``k_weight`` [D] (None: no norm); ``draft_mask`` as in
+    ``verify_attn_tree``.  Returns ``q_out`` (allocated if None; rows past a
+    chunk's end are left as they are).  ``q=None``: keys and values only,
+    returns None.
+    """
+    lib = load_library()
+    if k.dim() != 4 or k_cache.dim() != 4 or (q is not None and q.dim() != 4):
+        raise ValueError("q, k, v, k_cache and v_cache have four dimensions")
+    B, C_max, Hkv, D = k.shape
+    dt, dev = k.dtype, k.device
+    if rope not in ROPE_STYLES:
+        raise ValueError(f"rope must be one of {sorted(ROPE_STYLES)}, got {rope!r}")
+    paged = None
+    if block_table is None:
+        S_max = k_cache.shape[2]
+        shape = (B, Hkv, S_max, D)
+    else:
+        if block_table.dim() != 2:
+            raise ValueError("block_table must be [B, pages_per_seq]")
+        _check_on(block_table, "block_table", (B, block_table.shape[1]), torch.int32, dev)
+        num_pages, _, page_size, _ = k_cache.shape
+        paged = PagedKV(page_size, block_table.shape[1], num_pages)
+        S_max = page_size * block_table.shape[1]
+        shape = (num_pages, Hkv, page_size, D)
+    _check_on(k_cache, "k_cache", shape, dt, dev)
+    _check_on(v_cache, "v_cache", shape, dt, dev)
+    _check_on(ctx_lens, "ctx_lens", (B,), torch.int32, dev)
+    _check_on(chunk_lens, "chunk_lens", (B,), torch.int32, dev)
+    Hq = 0 if q is None else q.shape[2]
+    ks = _token_stride(k, "k", (B, C_max, Hkv, D), dt, dev)
+    vs = _token_stride(v, "v", (B, C_max, Hkv, D), dt, dev)
+    qs = 0
+    if q is not None:
+        qs = _token_stride(q, "q", (B, C_max, Hq, D), dt, dev)
+        if q_out is None:
+            q_out = _empty((B, C_max, Hq, D), dt, dev, stream)
+        else:
+            _check_on(q_out, "q_out", (B, C_max, Hq, D), dt, dev)
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _check_on(w, name, (D,), dt, dev)
+    rot_dim = 0
+    if inv_freq is not None:
+        _check_on(inv_freq, "inv_freq", (inv_freq.numel(),), torch.float64, dev)
+        rot_dim = 2 * inv_freq.numel()
+    if draft_mask is not None:
+        mdt = draft_mask.dtype if draft_mask.dtype in (torch.int64, torch.uint64) else torch.int64
+        _check_on(draft_mask, "draft_mask", (B, C_max), mdt, dev)
+    desc = AppendDesc(B, Hq, Hkv, D, C_max, S_max, _dtype_code(k), rot_dim, ROPE_STYLES[rope], eps, qs, ks, vs)
+    _launch(k, lib.specmoe_append_kv, _ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_weight), _ptr(k_weight),
+            _ptr(inv_freq), ctx_lens.data_ptr(), chunk_lens.data_ptr(), _ptr(draft_mask), _ptr(block_table),
+            _ptr(q_out) if q is not None else None, k_cache.data_ptr(), v_cache.data_ptr(), _raw_stream(k, stream),
+            ctypes.byref(desc), None if paged is None else ctypes.byref(paged))
+    return q_out if q is not None else None
+
+
+# ----------------------------------------------------------------- sampling
+
+def _sampling(n: int, device, temperature, top_k, top_p, min_p) -> Sampling:
+    for t, name, dt in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
+                        (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
+        if t is not None:
+            _check_on(t, name, (n,), dt, device)
+    return Sampling(_ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p))
+
+
+def sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+           top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+           min_p: Optional[torch.Tensor] = None, out=None, stream: Optional[torch.cuda.Stream] = None):
+    """One token per row of logits from given random numbers; see
+    ``specmoe_sample`` in ``include/specmoe_sample.h``.
+
+    logits [N, V] (bf16 or f32; rows may lie apart), uniforms float32 [N] in
+    [0, 1); the settings [N] (float32, top_k int32), None: off.  Returns
+    (tokens int32 [N], logprobs float32 [N]); ``out`` may supply the pair.
+    """
+    lib = load_library()
+    if logits.dim() != 2:
+        raise ValueError("logits must be [N, V]")
+    N, V = logits.shape
+    dev = logits.device
+    if not logits.is_cuda:
+        raise ValueError("logits must be a GPU tensor")
+    if V > 1 and logits.stride(1) != 1:
+        raise ValueError("the entries of a row of logits must lie side by side")
+    stride = logits.stride(0) if N > 1 else V
+    _check_on(uniforms, "uniforms", (N,), torch.float32, dev)
+    settings = _sampling(N, dev, temperature, top_k, top_p, min_p)
+    if out is None:
+        out = (_empty((N,), torch.int32, dev, stream), _empty((N,), torch.float32, dev, stream))
+    _check_on(out[0], "tokens", (N,), torch.int32, dev)
+    _check_on(out[1], "logprobs", (N,), torch.float32, dev)
+    desc = SampleDesc(N, V, _dtype_code(logits), 0, stride)
+    _launch(logits, lib.specmoe_sample, logits.data_ptr(), uniforms.data_ptr(), ctypes.byref(settings),
+            out[0].data_ptr(), out[1].data_ptr(), _raw_stream(logits, stream), ctypes.byref(desc))
+    return out[0], out[1]
+
+
+def accept_sample(logits: torch.Tensor, tokens: torch.Tensor, ctx_lens: torch.Tensor, chunk_lens: torch.Tensor,
+                  uniforms: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+                  top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                  min_p: Optional[torch.Tensor] = None, out: Optional[dict] = None,
+                  workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None,
+                  in_place: bool = False, _tree=None):
+    """Acceptance of draft tokens by sampling; see ``specmoe_accept_sample`` in
+    ``include/specmoe_sample.h``.
+
+    As ``accept_greedy`` (whose workspace it takes), plus uniforms float32
+    [B, C_max] and each sequence's settings [B] (None: off).  Returns a dict:
+    sampled int32 [B, C_max], logprobs float32 [B, C_max], accepted,
+    next_token and new_ctx_lens int32 [B].
+    """
+    lib = load_library()
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B, C_max, V]")
+    B, C_max, V = logits.shape
+    dev = logits.device
+    _check(logits, "logits", (B, C_max, V), logits.dtype)
+    _check_on(tokens, "tokens", (B, C_max), torch.int32, dev)
+    _check_on(ctx_lens, "ctx_lens", (B,), torch.int32, dev)
+    _check_on(chunk_lens, "chunk_lens", (B,), torch.int32, dev)
+    _check_on(uniforms, "uniforms", (B, C_max), torch.float32, dev)
+    settings = _sampling(B, dev, temperature, top_k, top_p, min_p)
+    out = {} if out is None else out
+    if in_place:
+        out["new_ctx_lens"] = ctx_lens
+    kinds = {"sampled": ((B, C_max), torch.int32), "logprobs": ((B, C_max), torch.float32),
+             "accepted": ((B,), torch.int32), "next_token": ((B,), torch.int32), "new_ctx_lens": ((B,), torch.int32)}
+    if _tree is not None:
+        kinds["path"] = ((B,), torch.int64)
+    for key, (shape, dt) in kinds.items():
+        if key not in out:
+            out[key] = _empty(shape, dt, dev, stream)
+        _check_on(out[key], key, shape, dt, dev)
+    desc = accept_desc(B, C_max, V, _dtype_code(logits))
+    if B == 0:
+        return out
+    if workspace is None:
+        workspace = alloc_accept_workspace(desc, dev, stream)
+    desc.workspace = workspace.data_ptr()
+    desc.workspace_bytes = workspace.nbytes
+    head = (logits.data_ptr(), tokens.data_ptr())
+    lens = (ctx_lens.data_ptr(), chunk_lens.data_ptr(), uniforms.data_ptr(), ctypes.byref(settings),
+            out["sampled"].data_ptr(), out["logprobs"].data_ptr(), out["accepted"].data_ptr(),
+            out["next_token"].data_ptr(), out["new_ctx_lens"].data_ptr())
+    tail = (_raw_stream(logits, stream), ctypes.byref(desc))
+    if _tree is None:
+        _launch(logits, lib.specmoe_accept_sample, *head, *lens, *tail)
+    else:
+        _launch(logits, lib.specmoe_accept_sample_tree, *head, _tree.data_ptr(), *lens, out["path"].data_ptr(), *tail)
+    return out
+
+
+def accept_sample_tree(logits: torch.Tensor, tokens: torch.Tensor, draft_mask: torch.Tensor, ctx_lens: torch.Tensor,
+                       chunk_lens: torch.Tensor, uniforms: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+                       top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                       min_p: Optional[torch.Tensor] = None, out: Optional[dict] = None,
+                       workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None,
+                       in_place: bool = False):
+    """Acceptance of tree drafts by sampling; see ``specmoe_accept_sample_tree``
+    in ``include/specmoe_sample.h``.  As ``accept_sample`` plus ``draft_mask``
+    (int64 [B, C_max] root-path words, C_max <= 64); the result also holds
+    ``path`` (int64 [B]) for ``compact_accepted_kv``."""
+    mdt = draft_mask.dtype if draft_mask.dtype in (torch.int64, torch.uint64) else torch.int64
+    _check_on(draft_mask, "draft_mask", tuple(tokens.shape), mdt, logits.device)
+    return accept_sample(logits, tokens, ctx_lens, chunk_lens, uniforms, temperature, top_k, top_p, min_p, out=out,
+                         workspace=workspace, stream=stream, in_place=in_place, _tree=draft_mask)

@@ -11,10 +11,12 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = [os.path.join(HERE, "csrc", "verify_attn.hip"), os.path.join(HERE, "csrc", "accept.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("verify_attn.hip", "accept.hip", "append.hip", "sample.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 OUTPUT = os.path.join(HERE, "libspecmoe_verify.so")
 PROBE_SOURCES = [os.path.join(HERE, "csrc", "stream_probe.hip")]
@@ -29,10 +31,14 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found")
 
 
-def build_command(output: str = OUTPUT, extra=(), sources=SOURCES):
-    return [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",
+def compile_command(source: str, output: str, extra=()):
+    return [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-c",
             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-            f"-I{INCLUDE}", *extra, *sources, "-o", output]
+            f"-I{INCLUDE}", *extra, source, "-o", output]
+
+
+def link_command(objects, output: str):
+    return [hipcc(), f"--offload-arch={ARCH}", "-fPIC", "-shared", *objects, "-o", output]
 
 
 def build(verbose: bool = False, output: str = OUTPUT) -> str:
@@ -43,9 +49,7 @@ def build(verbose: bool = False, output: str = OUTPUT) -> str:
     return output
 
 
-def _compile(sources, output: str, verbose: bool) -> None:
-    tmp = output + ".tmp"
-    cmd = build_command(tmp, sources=sources)
+def _run(cmd, verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -55,6 +59,16 @@ def _compile(sources, output: str, verbose: bool) -> None:
         raise RuntimeError(f"hipcc failed ({res.returncode}):\n{err}")
     if verbose and err.strip():
         print(err, file=sys.stderr)
+
+
+def _compile(sources, output: str, verbose: bool) -> None:
+    """Compile the sources side by side, link them and check the result."""
+    tmp = output + ".tmp"
+    with tempfile.TemporaryDirectory() as objdir:
+        objects = [os.path.join(objdir, os.path.basename(s) + ".o") for s in sources]
+        with ThreadPoolExecutor() as pool:
+            list(pool.map(lambda so: _run(compile_command(*so), verbose), zip(sources, objects)))
+        _run(link_command(objects, tmp), verbose)
     # every symbol must resolve: a kernel template whose host-side stub the
     # compiler silently failed to emit links fine but cannot be loaded
     check = subprocess.run([sys.executable, "-c", f"import ctypes; ctypes.CDLL({tmp!r})"],

@@ -29,26 +29,18 @@
 #include <math.h>
 #include <stdint.h>
 
+#include "accept_plan.h"
 #include "specmoe_accept.h"
 
 namespace {
 
-constexpr int kWavesPerGroup = 8;
 constexpr int kThreads = 64 * kWavesPerGroup;
-constexpr int kGroupsPerCU = 2;
-constexpr int kCUs = 256;                  // MI355X
-constexpr int kVecBytes = 16;
-constexpr int kItemBytes = 8192;           // default item: 8 KB of logits
 // 16-byte loads per lane in flight: 8 for waves with at least two default
 // items to read (B = 256, 131 MB: 24.6 us against 25.1 with 4 and 25.6 with
 // 2), 4 for the others, whose one item ends sooner the sooner its first half
 // is compared (B = 64, 20 MB: 8.8 us against 9.1 with 8).
 constexpr int kLongBatch = 8, kShortBatch = 4;
-constexpr int kSplitUnit = 512;            // item granularity (entries)
 constexpr int kModeIeee = 1 | (9 << 6);    // s_setreg operand: bit 9 of the MODE register
-constexpr int kMaxChunk = 1024;            // C_max limit
-constexpr int kMaxSeqs = 65536;            // B limit (fixed counter region)
-constexpr int kGroupSeqs = 16;             // sequences a workgroup counts through LDS
 // Partial results go through, or around, the XCD-local L2 to where every XCD
 // sees them (device scope), without an L2-wide write-back.
 constexpr int kDeviceCoherent = 16;        // SC1
@@ -393,51 +385,6 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kernel(char* k, char*
 __global__ void zero_kernel(int* x, int n) {
   const int i = blockIdx.x * blockDim.x + threadIdx.x;
   if (i < n) x[i] = 0;
-}
-
-size_t align256(size_t x) { return (x + 255) / 256 * 256; }
-
-int elt_of(const specmoe_accept_desc* d) { return d->dtype == SPECMOE_BF16 ? 2 : 4; }
-
-int split_of(const specmoe_accept_desc* d) { return d->split ? d->split : kItemBytes / elt_of(d); }
-
-int validate(const specmoe_accept_desc* d) {
-  if (!d) return SPECMOE_ERR_NULL_POINTER;
-  if (d->dtype != SPECMOE_F32 && d->dtype != SPECMOE_BF16) return SPECMOE_ERR_DTYPE;
-  if (d->flags != 0) return SPECMOE_ERR_FLAGS;
-  if (d->B < 0 || d->B > kMaxSeqs || d->C_max < 1 || d->C_max > kMaxChunk || d->V < 1) return SPECMOE_ERR_SHAPE;
-  const int64_t elt = elt_of(d);
-  if ((d->V * elt) % kVecBytes != 0) return SPECMOE_ERR_SHAPE;
-  if (d->split < 0 || d->split % kSplitUnit != 0) return SPECMOE_ERR_SHAPE;
-  const int64_t S = (d->V + (int64_t)split_of(d) - 1) / split_of(d);
-  // row offsets in elements, item indices and partial offsets in bytes stay
-  // in 32 bits
-  if ((int64_t)d->B * d->C_max * d->V >= ((int64_t)1 << 31)) return SPECMOE_ERR_SHAPE;
-  if ((int64_t)d->B * d->C_max * S * 8 >= ((int64_t)1 << 31)) return SPECMOE_ERR_SHAPE;
-  return SPECMOE_OK;
-}
-
-struct Plan {
-  int S, N, q, groups, grouped;
-  size_t counter_bytes, part_off, bytes;
-};
-
-Plan make_plan(const specmoe_accept_desc* d) {
-  Plan pl;
-  pl.S = (d->V + split_of(d) - 1) / split_of(d);
-  pl.N = d->B * d->C_max * pl.S;
-  // contiguous ranges of q items for at most the persistent grid's waves
-  const int waves = kCUs * kGroupsPerCU * kWavesPerGroup;
-  pl.q = pl.N > 0 ? (pl.N + waves - 1) / waves : 1;
-  const int used = pl.N > 0 ? (pl.N + pl.q - 1) / pl.q : 0;
-  pl.groups = (used + kWavesPerGroup - 1) / kWavesPerGroup;
-  // a range of gq items meets at most (gq - 1) / CS + 2 sequences
-  const int64_t gq = (int64_t)kWavesPerGroup * pl.q, CS = (int64_t)d->C_max * pl.S;
-  pl.grouped = (gq - 1) / CS + 2 <= kGroupSeqs;
-  pl.counter_bytes = align256((size_t)kMaxSeqs * sizeof(int));
-  pl.part_off = pl.counter_bytes;
-  pl.bytes = pl.part_off + (size_t)pl.N * 8;
-  return pl;
 }
 
 bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
