@@ -19,7 +19,8 @@
  * Entry points: specmoe_verify_attn (chain drafts, the mask above),
  * specmoe_verify_attn_tree (tree drafts: the draft part of the mask given as
  * one bit word per draft token), specmoe_verify_attn_paged (either, over a
- * paged KV cache).  q, k and v may be float32, bfloat16 or float16 (the
+ * paged KV cache), specmoe_verify_attn_scored (any of them, with capped,
+ * biased or windowed scores).  q, k and v may be float32, bfloat16 or float16 (the
  * paper's KV precision, Section 3.3).  The acceptance step that follows
  * verification is in specmoe_accept.h.
  *
@@ -36,7 +37,8 @@
 extern "C" {
 #endif
 
-/* Element type of q, k_cache and v_cache.  out and lse are always float32.
+/* Element type of q, k_cache and v_cache.  lse is always float32, and so is out
+ * except for specmoe_verify_attn_scored.
  * FP16 is the KV precision the paper assumes (Section 3.3, Section 6.1). */
 typedef enum {
   SPECMOE_F32 = 0,
@@ -270,6 +272,53 @@ int specmoe_verify_attn_paged(const void* q, const void* k_pages, const void* v_
                               const int32_t* chunk_lens, const uint64_t* draft_mask, float scale,
                               float* out, float* lse, void* stream, const specmoe_verify_desc* desc,
                               const specmoe_paged_kv* paged);
+
+/* What specmoe_verify_attn_scored does with the scores (host struct). */
+typedef struct specmoe_score {
+  float softcap;          /* > 0: scores become softcap * tanh(score / softcap); 0: off  */
+  int32_t window;         /* > 0: keys at a distance of window or more are hidden; 0: off */
+  const float* slopes;    /* device, float32 [Hq], or NULL: slope times the distance is
+                             taken off the scores of head h                              */
+  const int32_t* starts;  /* device, int32 [B], or NULL: keys before start_b are hidden  */
+} specmoe_score;
+
+/*
+ * specmoe_verify_attn_scored -- verification attention for models whose scores
+ * are not the plain products: the step of specmoe_verify_attn (or _tree, or
+ * _paged) with
+ *
+ *     s_ij = cap(scale q_i.k_j) - slope_h * dist(i, j),
+ *     cap(x) = softcap * tanh(x / softcap), or x without a softcap,
+ *
+ * over the keys j that the chain or draft mask shows to draft token i and that
+ * lie at j >= start_b and, with a window, at dist(i, j) < window.  The distance
+ * is the number of keys after j that the token sees: l_b + i - j for chains;
+ * for trees, a draft token's distance is counted along its path, and the one
+ * of a cached key is (l_b - 1 - j) + max(seen, 1), seen being the draft tokens
+ * in its word.  (Positions as specmoe_append_kv assigns them.)
+ *
+ *   q, k_cache, v_cache, ctx_lens, chunk_lens, scale, lse, stream, desc
+ *                as in specmoe_verify_attn; block_table and paged as in
+ *                specmoe_verify_attn_paged, or both NULL for a contiguous
+ *                cache; draft_mask as in specmoe_verify_attn_tree, or NULL.
+ *   out          device, 16-byte aligned: [B, C_max, Hq, D] of desc's dtype
+ *                (the type that the projection after it takes).
+ *   score        host pointer to the settings; any of them may be off.
+ *
+ * A token that sees no key gets out = 0 and lse = -inf, as padding rows do.
+ * Keys before max(start_b, l_b + 1 - window) are never read, nor are the table
+ * entries of pages that hold only such keys.  start_b is clamped into
+ * [0, l_b]: the chunk's own keys stay.
+ *
+ * The workspace is that of specmoe_verify_attn and can be shared with it; the
+ * preconditions, ownership and determinism are the same.  Errors are those of
+ * specmoe_verify_attn_paged; SPECMOE_ERR_SCORE reports a bad softcap or window,
+ * SPECMOE_ERR_NULL_POINTER a NULL score or a table without its geometry.
+ */
+int specmoe_verify_attn_scored(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_table,
+                               const int32_t* ctx_lens, const int32_t* chunk_lens, const uint64_t* draft_mask,
+                               float scale, void* out, float* lse, void* stream, const specmoe_verify_desc* desc,
+                               const specmoe_paged_kv* paged, const specmoe_score* score);
 
 /* Bytes of device workspace specmoe_verify_attn needs for `desc` (its
  * grid_blocks included); 0 for an invalid descriptor.  The workspace starts

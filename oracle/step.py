@@ -62,11 +62,13 @@ def append_ref(q, k, v, k_cache, v_cache, q_out, ctx_lens, chunk_lens, inv_freq=
     return q_out, k_cache, v_cache
 
 
-def scored_row_ref(q, k, v, scale, sees, softcap=0.0, slope=0.0, window=0, start=0):
+def scored_row_ref(q, k, v, scale, sees, softcap=0.0, slope=0.0, window=0, start=0, l=None):
     """Output and log-sum-exp of one query over T keys; ``sees`` the keys that
-    the mask shows it."""
+    the mask shows it, the first ``l`` of them cached (None: all but one)."""
     T = k.shape[0]
-    dist = np.array([int(sees[j + 1:].sum()) for j in range(T)])
+    dist = sees.sum() - np.cumsum(sees)   # the keys after each that it sees (for a key it does not see: unused)
+    if l is not None and not sees[l:].any():
+        dist = dist + 1                   # a token that sees no draft token stands like a root
     s = (k @ q) * scale
     if softcap:
         s = softcap * np.tanh(s / softcap)
@@ -98,7 +100,7 @@ def scored_attn_ref(q, k_cache, v_cache, ctx_lens, chunk_lens, scale, softcap=0.
             for h in range(Hq):
                 out[b, i, h], lse[b, i, h] = scored_row_ref(
                     q[b, i, h], k_cache[b, h // g, :T], v_cache[b, h // g, :T], scale, sees, softcap,
-                    0.0 if slopes is None else float(slopes[h]), window, 0 if starts is None else int(starts[b]))
+                    0.0 if slopes is None else float(slopes[h]), window, 0 if starts is None else int(starts[b]), l)
     return out, lse
 
 

@@ -65,6 +65,12 @@ class AppendDesc(ctypes.Structure):
     ]
 
 
+class Score(ctypes.Structure):
+    """Mirror of ``specmoe_score``."""
+    _fields_ = [("softcap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p),
+                ("starts", ctypes.c_void_p)]
+
+
 class SampleDesc(ctypes.Structure):
     """Mirror of ``specmoe_sample_desc``."""
     _fields_ = [("N", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_int32),
@@ -129,6 +135,10 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.specmoe_accept_workspace_init.restype = ctypes.c_int
     lib.specmoe_accept_workspace_init.argtypes = [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p,
                                                   ctypes.POINTER(AcceptDesc)]
+    lib.specmoe_verify_attn_scored.restype = ctypes.c_int
+    lib.specmoe_verify_attn_scored.argtypes = [ctypes.c_void_p] * 7 + [
+        ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(Desc),
+        ctypes.POINTER(PagedKV), ctypes.POINTER(Score)]
     lib.specmoe_append_kv.restype = ctypes.c_int
     lib.specmoe_append_kv.argtypes = [ctypes.c_void_p] * 14 + [ctypes.POINTER(AppendDesc), ctypes.POINTER(PagedKV)]
     lib.specmoe_sample.restype = ctypes.c_int
@@ -631,6 +641,89 @@ def append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, k_cac
             _ptr(q_out) if q is not None else None, k_cache.data_ptr(), v_cache.data_ptr(), _raw_stream(k, stream),
             ctypes.byref(desc), None if paged is None else ctypes.byref(paged))
     return q_out if q is not None else None
+
+
+# --------------------------------------------------------- scored attention
+
+def _scored_shape(q: torch.Tensor, k_cache: torch.Tensor, block_table: Optional[torch.Tensor]):
+    """(Hkv, S_max, page geometry or None) of a contiguous or paged cache."""
+    if q.dim() != 4 or k_cache.dim() != 4:
+        raise ValueError("q must be [B, C_max, Hq, D], k_cache [B, Hkv, S_max, D] or [num_pages, Hkv, page_size, D]")
+    if block_table is None:
+        return k_cache.shape[1], k_cache.shape[2], None
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, pages_per_seq]")
+    paged = PagedKV(k_cache.shape[2], block_table.shape[1], k_cache.shape[0])
+    return k_cache.shape[1], paged.page_size * paged.pages_per_seq, paged
+
+
+def alloc_scored_workspace(q: torch.Tensor, k_cache: torch.Tensor, block_table: Optional[torch.Tensor] = None,
+                           grid_blocks: int = 0, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """A workspace for ``verify_attn_scored`` calls of these shapes (one of
+    ``alloc_workspace``, which serves ``verify_attn`` too)."""
+    B, C_max, Hq, D = q.shape
+    Hkv, S_max, _ = _scored_shape(q, k_cache, block_table)
+    return alloc_workspace(make_desc(B, Hq, Hkv, D, C_max, S_max, _dtype_code(q), grid_blocks), q.device, stream)
+
+
+def verify_attn_scored(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, ctx_lens: torch.Tensor,
+                       chunk_lens: torch.Tensor, scale: float, softcap: float = 0.0,
+                       slopes: Optional[torch.Tensor] = None, window: int = 0,
+                       starts: Optional[torch.Tensor] = None, draft_mask: Optional[torch.Tensor] = None,
+                       block_table: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                       lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                       grid_blocks: int = 0, stream: Optional[torch.cuda.Stream] = None, flags: int = 0,
+                       check_lengths: bool = False):
+    """Verification attention with capped, biased or windowed scores; see
+    ``specmoe_verify_attn_scored`` in ``include/specmoe_verify.h``.
+
+    Arguments as ``verify_attn``, ``verify_attn_tree`` (``draft_mask``) and
+    ``verify_attn_paged`` (``block_table``); ``softcap`` (0: off), ``window``
+    in keys (0: off), ``slopes`` float32 [Hq] and ``starts`` int32 [B] on the
+    GPU (None: off).  Returns (out, lse): ``out`` [B, C_max, Hq, D] in q's
+    type, ``lse`` float32 [B, C_max, Hq].
+    """
+    lib = load_library()
+    Hkv, S_max, paged = _scored_shape(q, k_cache, block_table)
+    B, C_max, Hq, D = q.shape
+    dt, dev = q.dtype, q.device
+    _check(q, "q", (B, C_max, Hq, D), dt)
+    cache = (B, Hkv, S_max, D) if paged is None else (paged.num_pages, Hkv, paged.page_size, D)
+    _check_on(k_cache, "k_cache", cache, dt, dev)
+    _check_on(v_cache, "v_cache", cache, dt, dev)
+    _check_on(ctx_lens, "ctx_lens", (B,), torch.int32, dev)
+    _check_on(chunk_lens, "chunk_lens", (B,), torch.int32, dev)
+    if block_table is not None:
+        _check_on(block_table, "block_table", (B, block_table.shape[1]), torch.int32, dev)
+    if slopes is not None:
+        _check_on(slopes, "slopes", (Hq,), torch.float32, dev)
+    if starts is not None:
+        _check_on(starts, "starts", (B,), torch.int32, dev)
+    if draft_mask is not None:
+        mdt = draft_mask.dtype if draft_mask.dtype in (torch.int64, torch.uint64) else torch.int64
+        _check_on(draft_mask, "draft_mask", (B, C_max), mdt, dev)
+    if check_lengths:
+        c, l = chunk_lens.cpu(), ctx_lens.cpu()
+        if (c < 0).any() or (c > C_max).any() or (l < 0).any() or (l + c > S_max).any():
+            raise ValueError("lengths break 0 <= c_b <= C_max, l_b >= 0, l_b + c_b <= S_max")
+    if out is None:
+        out = _empty((B, C_max, Hq, D), dt, dev, stream)
+    if lse is None:
+        lse = _empty((B, C_max, Hq), torch.float32, dev, stream)
+    _check_on(out, "out", (B, C_max, Hq, D), dt, dev)
+    _check_on(lse, "lse", (B, C_max, Hq), torch.float32, dev)
+    desc = make_desc(B, Hq, Hkv, D, C_max, S_max, _dtype_code(q), grid_blocks, flags)
+    if B > 0:
+        if workspace is None:
+            workspace = alloc_workspace(desc, dev, stream)
+        desc.workspace = workspace.data_ptr()
+        desc.workspace_bytes = workspace.nbytes
+    score = Score(softcap, window, _ptr(slopes), _ptr(starts))
+    _launch(q, lib.specmoe_verify_attn_scored, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+            _ptr(block_table), ctx_lens.data_ptr(), chunk_lens.data_ptr(), _ptr(draft_mask), float(scale),
+            out.data_ptr(), lse.data_ptr(), _raw_stream(q, stream), ctypes.byref(desc),
+            None if paged is None else ctypes.byref(paged), ctypes.byref(score))
+    return out, lse
 
 
 # ----------------------------------------------------------------- sampling

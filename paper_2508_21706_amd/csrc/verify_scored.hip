@@ -1,0 +1,44 @@
+// Verification attention with scores of their own (capped, lowered with the
+// distance, hidden by a window or a first key) for MI355X (gfx950, CDNA4): the
+// kernel of verify_kernel.h with the scores' changes compiled in, so the calls
+// without them keep theirs.
+//
+// The changes cost the consumer waves a few instructions per score and the
+// stream nothing; what a window or a first key hides from all of a sequence's
+// tokens is neither loaded nor scheduled.
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+#include <stdint.h>
+
+#include "specmoe_verify.h"
+#include "verify_kernel.h"
+
+extern "C" int specmoe_verify_attn_scored(const void* q, const void* k_cache, const void* v_cache,
+                                          const int32_t* block_table, const int32_t* ctx_lens,
+                                          const int32_t* chunk_lens, const uint64_t* draft_mask, float scale, void* out,
+                                          float* lse, void* stream, const specmoe_verify_desc* desc,
+                                          const specmoe_paged_kv* paged, const specmoe_score* score) {
+  if (!score) return SPECMOE_ERR_NULL_POINTER;
+  const bool tree = draft_mask != nullptr;
+  int st = validate_call(desc, tree, paged);
+  if (st != SPECMOE_OK) return st;
+  if (!(score->softcap >= 0.f) || !isfinite(score->softcap) || score->window < 0) return SPECMOE_ERR_SCORE;
+  if (block_table && !paged) return SPECMOE_ERR_NULL_POINTER;
+  if (desc->B == 0) return SPECMOE_OK;   // nothing to read or write
+  ScoredParams p;
+  Plan pl;
+  st = make_params(q, k_cache, v_cache, ctx_lens, chunk_lens, draft_mask, tree, scale, out, lse, desc, block_table,
+                   paged, p, pl);
+  if (st != SPECMOE_OK) return st;
+  if ((reinterpret_cast<uintptr_t>(score->slopes) | reinterpret_cast<uintptr_t>(score->starts)) & 3u)
+    return SPECMOE_ERR_ALIGN;
+  p.cap_in = score->softcap > 0.f ? scale / score->softcap : 0.f;
+  p.cap2 = score->softcap * kLog2e;
+  p.slopes = score->slopes;
+  p.starts = score->starts;
+  p.window = score->window;
+  (void)hipGetLastError();  // clear a stale error from unrelated work
+  launch_for<true>(desc->dtype, desc->D, tree, paged != nullptr, p, pl, static_cast<hipStream_t>(stream));
+  return hipGetLastError() == hipSuccess ? SPECMOE_OK : SPECMOE_ERR_LAUNCH;
+}

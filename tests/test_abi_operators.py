@@ -22,6 +22,7 @@ def lib():
 
 @pytest.mark.parametrize("header,struct,mirror", [
     ("specmoe_append.h", "specmoe_append_desc", bd.AppendDesc),
+    ("specmoe_verify.h", "specmoe_score", bd.Score),
     ("specmoe_sample.h", "specmoe_sample_desc", bd.SampleDesc),
     ("specmoe_sample.h", "specmoe_sampling", bd.Sampling),
 ])
@@ -148,6 +149,48 @@ def test_accept_sample_refusals(lib):
     assert accept(lib, desc(), FAKE, path=None) == -1
     assert accept(lib, desc(), FAKE + 4) == -9
     assert accept(lib, desc(), FAKE, path=FAKE + 4) == -9
+
+
+SCORED = ["q", "k", "v", "table", "ctx", "chunk", "mask", "scale", "out", "lse"]
+
+
+def scored(lib, desc, score=bd.Score(30.0, 0, None, None), paged=None, **kw):
+    args = dict.fromkeys(SCORED, FAKE)
+    args.update(mask=None, table=None if paged is None else FAKE, scale=0.088)
+    args.update(kw)
+    ref = lambda s: None if s is None else ctypes.byref(s)   # noqa: E731
+    return lib.specmoe_verify_attn_scored(*(args[n] for n in SCORED), None, ref(desc), ref(paged), ref(score))
+
+
+def test_scored_refusals(lib):
+    def desc(**kw):
+        d = bd.make_desc(**dict(dict(B=2, Hq=32, Hkv=8, D=128, C_max=5, S_max=2304, dtype=1), **kw))
+        d.workspace, d.workspace_bytes = FAKE, 1 << 30
+        return d
+    assert scored(lib, None) == -1
+    assert scored(lib, desc(), None) == -1
+    for kw, code in ((dict(dtype=7), -5), (dict(D=96), -4), (dict(B=-1), -2), (dict(Hq=30), -3),
+                     (dict(C_max=33), -6), (dict(grid_blocks=4000), -7), (dict(flags=2), -12)):
+        assert scored(lib, desc(**kw)) == code, kw
+    for n in ("q", "k", "v", "ctx", "chunk", "out", "lse"):
+        assert scored(lib, desc(), **{n: None}) == -1, n
+    for n in ("q", "k", "v", "out"):
+        assert scored(lib, desc(), **{n: FAKE + 8}) == -9, n
+    assert scored(lib, desc(), mask=FAKE + 4) == -9
+    assert scored(lib, desc(Hq=8, C_max=65), mask=FAKE) == -13
+    assert scored(lib, desc(), scale=-1.0) == -10
+    for cap, window in ((-1.0, 0), (float("nan"), 0), (float("inf"), 0), (1.0, -1)):
+        assert scored(lib, desc(), bd.Score(cap, window, None, None)) == -17
+        assert scored(lib, desc(B=0), bd.Score(cap, window, None, None)) == -17
+    assert scored(lib, desc(), bd.Score(0.0, 0, FAKE + 2, None)) == -9
+    assert scored(lib, desc(), bd.Score(0.0, 0, None, FAKE + 1)) == -9
+    assert scored(lib, desc(), table=FAKE) == -1
+    assert scored(lib, desc(), paged=bd.PagedKV(16, 144, 9), table=None) == -1
+    assert scored(lib, desc(), paged=bd.PagedKV(16, 143, 9)) == -14
+    d = desc()
+    d.workspace_bytes = 64
+    assert scored(lib, d) == -8
+    assert scored(lib, desc(B=0), q=None, out=None) == 0
 
 
 def test_binding_refuses_host_tensors_and_wrong_shapes():
