@@ -293,3 +293,26 @@ def test_distribution_of_accepted_tokens():
     p = torch.softmax(logits[0, 0].double(), 0)
     # a share's standard deviation is at most 0.5 / sqrt(N); six of them
     assert (share - p).abs().max() < 6 * 0.5 / N ** 0.5
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_bins_around_zero_and_far_apart(dtype):
+    """Rows whose numbers have more patterns than there are bins: many around 0,
+    of one sign, of far apart sizes, and infinities beside NaN."""
+    V, N = 6000, 8
+    gen = torch.Generator().manual_seed(21)
+    z = torch.randn((N, V), generator=gen)
+    u = torch.rand((N,), generator=gen).numpy()
+    rows = {"small": z * 1e-3, "tiny": z * 1e-30, "sizes": z.sign() * 10.0 ** (z.abs() * 8 - 12),
+            "negative": -10.0 ** (z * 3), "positive": 10.0 ** (z * 3 - 6), "wide": z.sign() * 10.0 ** (z.abs() * 12 - 10)}
+    near = z.clone()
+    near[:, ::2] *= 2.0 ** -20
+    rows["half near 0"] = near
+    mixed = z.clone()
+    mixed[:, ::5], mixed[:, 1::7] = float("inf"), float("nan")
+    rows["infinities"] = mixed
+    for name, x in rows.items():
+        x = x.to(TYPES[dtype]).to(dev())
+        for kw in ({}, dict(temperature=[30.0] * N), dict(temperature=[1e6] * N), dict(top_k=[700] * N, top_p=[0.8] * N),
+                   dict(top_k=[60] * N), dict(min_p=[0.4] * N, temperature=[5.0] * N)):
+            check_rows(x, u, **kw, label=f"{dtype} {name} {str(kw)[:24]}")
