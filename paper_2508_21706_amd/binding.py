@@ -537,18 +537,24 @@ def accept_greedy(logits: torch.Tensor, tokens: torch.Tensor, ctx_lens: torch.Te
 
 # ------------------------------------------------------------- chunk append
 
-def _check_on(t: torch.Tensor, name: str, shape, dtype, device):
+def _check_on(t: torch.Tensor, name: str, shape, dtype, gpu: int):
+    """``_check``, and that ``t`` is on GPU ``gpu`` (a tensor's get_device())."""
+    # (one expression again: these calls check a dozen tensors)
+    if t.dtype is dtype and t.get_device() == gpu and t.shape == shape and t.is_contiguous() and gpu >= 0:
+        return
     _check(t, name, shape, dtype)
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    raise ValueError(f"{name} is on {t.device}, expected cuda:{gpu}")
 
 
-def _launch(t: torch.Tensor, call, *args):
-    """A library call with ``t``'s GPU current; raises on an error status."""
-    if t.get_device() == torch.cuda.current_device():
+_current_gpu = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _launch(gpu: int, call, *args):
+    """A library call with GPU ``gpu`` current; raises on an error status."""
+    if gpu == _current_gpu():
         st = call(*args)
     else:
-        with torch.cuda.device(t.device):
+        with torch.cuda.device(gpu):
             st = call(*args)
     if st != 0:
         raise SpecMoEError(st, status_str(st))
@@ -558,15 +564,15 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _token_stride(t: torch.Tensor, name: str, shape, dtype, device) -> int:
+def _token_stride(t: torch.Tensor, name: str, shape, dtype, gpu: int) -> int:
     """Elements from one token's row of ``t`` [B, C_max, H, D] to the next's;
     a row's heads lie side by side."""
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or t.device != device:
-        _check_on(t, name, shape, dtype, device)
+    if t.shape != shape or t.dtype is not dtype or gpu < 0 or t.get_device() != gpu:
+        _check_on(t.contiguous(), name, shape, dtype, gpu)
     B, C, H, D = shape
-    if t.is_contiguous():
-        return H * D
     sb, sc, sh, sd = t.stride()
+    if sc == H * D and sd == 1 and sh == D and sb == C * sc:
+        return sc
     stride = sc if C > 1 else sb if B > 1 else H * D
     if (D > 1 and sd != 1) or (H > 1 and sh != D) or (B > 1 and C > 1 and sb != C * sc):
         raise ValueError(f"{name} must be rows of side-by-side heads at one distance from token to token")
@@ -596,7 +602,7 @@ def append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, k_cac
     if k.dim() != 4 or k_cache.dim() != 4 or (q is not None and q.dim() != 4):
         raise ValueError("q, k, v, k_cache and v_cache have four dimensions")
     B, C_max, Hkv, D = k.shape
-    dt, dev = k.dtype, k.device
+    dt, dev = k.dtype, k.get_device()
     if rope not in ROPE_STYLES:
         raise ValueError(f"rope must be one of {sorted(ROPE_STYLES)}, got {rope!r}")
     paged = None
@@ -622,7 +628,7 @@ def append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, k_cac
     if q is not None:
         qs = _token_stride(q, "q", (B, C_max, Hq, D), dt, dev)
         if q_out is None:
-            q_out = _empty((B, C_max, Hq, D), dt, dev, stream)
+            q_out = _empty((B, C_max, Hq, D), dt, k.device, stream)
         else:
             _check_on(q_out, "q_out", (B, C_max, Hq, D), dt, dev)
     for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
@@ -636,7 +642,7 @@ def append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, k_cac
         mdt = draft_mask.dtype if draft_mask.dtype in (torch.int64, torch.uint64) else torch.int64
         _check_on(draft_mask, "draft_mask", (B, C_max), mdt, dev)
     desc = AppendDesc(B, Hq, Hkv, D, C_max, S_max, _dtype_code(k), rot_dim, ROPE_STYLES[rope], eps, qs, ks, vs)
-    _launch(k, lib.specmoe_append_kv, _ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_weight), _ptr(k_weight),
+    _launch(dev, lib.specmoe_append_kv, _ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_weight), _ptr(k_weight),
             _ptr(inv_freq), ctx_lens.data_ptr(), chunk_lens.data_ptr(), _ptr(draft_mask), _ptr(block_table),
             _ptr(q_out) if q is not None else None, k_cache.data_ptr(), v_cache.data_ptr(), _raw_stream(k, stream),
             ctypes.byref(desc), None if paged is None else ctypes.byref(paged))
@@ -686,8 +692,8 @@ def verify_attn_scored(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Te
     lib = load_library()
     Hkv, S_max, paged = _scored_shape(q, k_cache, block_table)
     B, C_max, Hq, D = q.shape
-    dt, dev = q.dtype, q.device
-    _check(q, "q", (B, C_max, Hq, D), dt)
+    dt, dev = q.dtype, q.get_device()
+    _check_on(q, "q", (B, C_max, Hq, D), dt, dev)
     cache = (B, Hkv, S_max, D) if paged is None else (paged.num_pages, Hkv, paged.page_size, D)
     _check_on(k_cache, "k_cache", cache, dt, dev)
     _check_on(v_cache, "v_cache", cache, dt, dev)
@@ -707,19 +713,19 @@ def verify_attn_scored(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Te
         if (c < 0).any() or (c > C_max).any() or (l < 0).any() or (l + c > S_max).any():
             raise ValueError("lengths break 0 <= c_b <= C_max, l_b >= 0, l_b + c_b <= S_max")
     if out is None:
-        out = _empty((B, C_max, Hq, D), dt, dev, stream)
+        out = _empty((B, C_max, Hq, D), dt, q.device, stream)
     if lse is None:
-        lse = _empty((B, C_max, Hq), torch.float32, dev, stream)
+        lse = _empty((B, C_max, Hq), torch.float32, q.device, stream)
     _check_on(out, "out", (B, C_max, Hq, D), dt, dev)
     _check_on(lse, "lse", (B, C_max, Hq), torch.float32, dev)
     desc = make_desc(B, Hq, Hkv, D, C_max, S_max, _dtype_code(q), grid_blocks, flags)
     if B > 0:
         if workspace is None:
-            workspace = alloc_workspace(desc, dev, stream)
+            workspace = alloc_workspace(desc, q.device, stream)
         desc.workspace = workspace.data_ptr()
         desc.workspace_bytes = workspace.nbytes
     score = Score(softcap, window, _ptr(slopes), _ptr(starts))
-    _launch(q, lib.specmoe_verify_attn_scored, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+    _launch(dev, lib.specmoe_verify_attn_scored, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
             _ptr(block_table), ctx_lens.data_ptr(), chunk_lens.data_ptr(), _ptr(draft_mask), float(scale),
             out.data_ptr(), lse.data_ptr(), _raw_stream(q, stream), ctypes.byref(desc),
             None if paged is None else ctypes.byref(paged), ctypes.byref(score))
@@ -750,8 +756,8 @@ def sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature: Optional[t
     if logits.dim() != 2:
         raise ValueError("logits must be [N, V]")
     N, V = logits.shape
-    dev = logits.device
-    if not logits.is_cuda:
+    dev = logits.get_device()
+    if dev < 0:
         raise ValueError("logits must be a GPU tensor")
     if V > 1 and logits.stride(1) != 1:
         raise ValueError("the entries of a row of logits must lie side by side")
@@ -759,11 +765,11 @@ def sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature: Optional[t
     _check_on(uniforms, "uniforms", (N,), torch.float32, dev)
     settings = _sampling(N, dev, temperature, top_k, top_p, min_p)
     if out is None:
-        out = (_empty((N,), torch.int32, dev, stream), _empty((N,), torch.float32, dev, stream))
+        out = (_empty((N,), torch.int32, logits.device, stream), _empty((N,), torch.float32, logits.device, stream))
     _check_on(out[0], "tokens", (N,), torch.int32, dev)
     _check_on(out[1], "logprobs", (N,), torch.float32, dev)
     desc = SampleDesc(N, V, _dtype_code(logits), 0, stride)
-    _launch(logits, lib.specmoe_sample, logits.data_ptr(), uniforms.data_ptr(), ctypes.byref(settings),
+    _launch(dev, lib.specmoe_sample, logits.data_ptr(), uniforms.data_ptr(), ctypes.byref(settings),
             out[0].data_ptr(), out[1].data_ptr(), _raw_stream(logits, stream), ctypes.byref(desc))
     return out[0], out[1]
 
@@ -786,8 +792,8 @@ def accept_sample(logits: torch.Tensor, tokens: torch.Tensor, ctx_lens: torch.Te
     if logits.dim() != 3:
         raise ValueError("logits must be [B, C_max, V]")
     B, C_max, V = logits.shape
-    dev = logits.device
-    _check(logits, "logits", (B, C_max, V), logits.dtype)
+    dev = logits.get_device()
+    _check_on(logits, "logits", (B, C_max, V), logits.dtype, dev)
     _check_on(tokens, "tokens", (B, C_max), torch.int32, dev)
     _check_on(ctx_lens, "ctx_lens", (B,), torch.int32, dev)
     _check_on(chunk_lens, "chunk_lens", (B,), torch.int32, dev)
@@ -802,13 +808,13 @@ def accept_sample(logits: torch.Tensor, tokens: torch.Tensor, ctx_lens: torch.Te
         kinds["path"] = ((B,), torch.int64)
     for key, (shape, dt) in kinds.items():
         if key not in out:
-            out[key] = _empty(shape, dt, dev, stream)
+            out[key] = _empty(shape, dt, logits.device, stream)
         _check_on(out[key], key, shape, dt, dev)
     desc = accept_desc(B, C_max, V, _dtype_code(logits))
     if B == 0:
         return out
     if workspace is None:
-        workspace = alloc_accept_workspace(desc, dev, stream)
+        workspace = alloc_accept_workspace(desc, logits.device, stream)
     desc.workspace = workspace.data_ptr()
     desc.workspace_bytes = workspace.nbytes
     head = (logits.data_ptr(), tokens.data_ptr())
@@ -817,9 +823,9 @@ def accept_sample(logits: torch.Tensor, tokens: torch.Tensor, ctx_lens: torch.Te
             out["next_token"].data_ptr(), out["new_ctx_lens"].data_ptr())
     tail = (_raw_stream(logits, stream), ctypes.byref(desc))
     if _tree is None:
-        _launch(logits, lib.specmoe_accept_sample, *head, *lens, *tail)
+        _launch(dev, lib.specmoe_accept_sample, *head, *lens, *tail)
     else:
-        _launch(logits, lib.specmoe_accept_sample_tree, *head, _tree.data_ptr(), *lens, out["path"].data_ptr(), *tail)
+        _launch(dev, lib.specmoe_accept_sample_tree, *head, _tree.data_ptr(), *lens, out["path"].data_ptr(), *tail)
     return out
 
 
@@ -834,6 +840,6 @@ def accept_sample_tree(logits: torch.Tensor, tokens: torch.Tensor, draft_mask: t
     (int64 [B, C_max] root-path words, C_max <= 64); the result also holds
     ``path`` (int64 [B]) for ``compact_accepted_kv``."""
     mdt = draft_mask.dtype if draft_mask.dtype in (torch.int64, torch.uint64) else torch.int64
-    _check_on(draft_mask, "draft_mask", tuple(tokens.shape), mdt, logits.device)
+    _check_on(draft_mask, "draft_mask", tuple(tokens.shape), mdt, logits.get_device())
     return accept_sample(logits, tokens, ctx_lens, chunk_lens, uniforms, temperature, top_k, top_p, min_p, out=out,
                          workspace=workspace, stream=stream, in_place=in_place, _tree=draft_mask)
