@@ -139,7 +139,7 @@ __global__ __launch_bounds__(kMaxThreads) void append_kernel(Params p) {
         int pos = l + i;
         if (p.draft_mask) {
           const uint64_t seen = p.draft_mask[token] & (c >= kMaxDraftBits ? ~0ull : (1ull << c) - 1);
-          pos = l + max(__popcll(seen), 1) - 1;
+          pos = l + max((int)__popcll(seen), 1) - 1;
         }
         // the angle in turns, less its whole turns: exact to 2^-53 of the
         // angle, so far positions lose nothing in fp32

@@ -22,6 +22,12 @@ static __device__ __attribute__((aligned(256))) char scratch[kScratchBytes];
 
 namespace {
 
+// Zero the per-unit counters of a workspace.
+__global__ void zero_counters_kernel(int* counters, int n) {
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < n) counters[i] = 0;
+}
+
 // Host checks and launch of both entry points; draft_mask is NULL for a
 // chain draft.
 int run(const void* q, const void* k_cache, const void* v_cache, const int32_t* ctx_lens,

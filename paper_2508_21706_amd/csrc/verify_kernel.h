@@ -957,9 +957,8 @@ __global__ __launch_bounds__(kThreads, 1) void verify_attn_kernel(ParamsOf<SCORE
   // would cover the Q prefetch and the stores issued before it
   uint64_t tm_r = 0, tm_n = 0;
   // (scored calls) the slope of the row's head in log2 units, of this
-  // segment's unit and of the next's, and the position of the row's token
-  float sl_r = 0.f, sl_n = 0.f, slope = 0.f;
-  int pos = 0;
+  // segment's unit and of the next's
+  float sl_r = 0.f, sl_n = 0.f;
   // x / g for a row 0 <= x < 128 of a unit, by a float reciprocal: exact
   // there, as (x + 1/2) / g lies at least 1 / (2 g) from an integer
   const float inv_g = 1.f / (float)g;
@@ -985,20 +984,14 @@ __global__ __launch_bounds__(kThreads, 1) void verify_attn_kernel(ParamsOf<SCORE
       // every key below the sequence end passes the compare; the draft
       // keys are then filtered by the row's word
       vis = 0x7fffffff;
-      tmask = tm_r;   // 0 for rows that are not valid
+      if constexpr (!SCORED) tmask = tm_r;   // 0 for rows that are not valid
     } else {
       vis = row_valid ? l_ctx + tok : 0x7fffffff;   // last visible key of this lane's row
     }
-    if constexpr (SCORED) {
-      slope = sl_r;
-      int seen = tok + 1;   // draft tokens that the row sees
-      if constexpr (TREE) {
-        tmask &= c >= 64 ? ~0ull : (1ull << c) - 1;
-        seen = max(__popcll(tmask), 1);
-      }
-      pos = l_ctx + seen - 1;
-    }
   };
+  // (scored calls) position of the row's token: worked out where it is used,
+  // for registers
+  auto position = [&]() { return l_ctx + (TREE ? max((int)__popcll(tm_r), 1) - 1 : tok); };
   // Q chunks of this lane's row for the unit of cu (zero for invalid rows):
   // chunk 4J + lg of the row feeds the J-th score MFMA.  Consumers only.
   auto load_q = [&](const Cursor& cu, u32x4* dst, uint64_t& mdst, float& sdst) {
@@ -1017,6 +1010,7 @@ __global__ __launch_bounds__(kThreads, 1) void verify_attn_kernel(ParamsOf<SCORE
     for (int J = 0; J < C::kQJ; ++J)
       dst[J] = ok ? *reinterpret_cast<const u32x4*>(qrow + 16 * (4 * J + lg)) : u32x4{0u, 0u, 0u, 0u};
     if constexpr (TREE) mdst = ok ? p.draft_mask[cu.b * p.C_max + tk] : 0;
+    if constexpr (TREE && SCORED) mdst &= c >= 64 ? ~0ull : (1ull << c) - 1;   // (the word counts drafts)
     if constexpr (SCORED) sdst = ok && p.slopes ? p.slopes[cu.kvh * g + row_ - tk * g] : 0.f;
   };
 
@@ -1033,6 +1027,11 @@ __global__ __launch_bounds__(kThreads, 1) void verify_attn_kernel(ParamsOf<SCORE
     int state;   // 0 stored, 1 counted, 2 no piece, 3 held in LDS
     int unit, v, rows;
   };
+
+  // (scored calls) what a score is multiplied with in the exponential
+  float x_scale = 1.f;
+  if constexpr (SCORED)
+    if (p.cap_in == 0.f && !p.slopes) x_scale = p.sl2;
 
   // ---- consumers.  Per-segment state of a lane: O^T blocks, running max
   // (log2 units, the same in the four lanes of a row), this lane's share of
@@ -1294,30 +1293,36 @@ __global__ __launch_bounds__(kThreads, 1) void verify_attn_kernel(ParamsOf<SCORE
                   (lds_i16x4*)(__attribute__((address_space(3))) char*)(vrow + h * vbstride + 32 * db));
         }
 
-        // mask, online softmax over the pair's keys (x: unscaled scores; in
-        // scored calls, scores in log2 units)
+        // mask, online softmax over the pair's keys (x: unscaled scores, or
+        // in scored calls with a cap or slopes, scores in log2 units)
         float x[8];
         float mx = -INFINITY;
         if constexpr (SCORED) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = sa[e >> 2][e & 3];
-          if (p.cap_in > 0.f) {
-            cap_scores(p, x);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] *= p.sl2;
-          }
+          if (p.cap_in > 0.f) cap_scores(p, x);
+          // a key's distance: in the context, and for chains, the positions'
+          // difference; for a tree's draft key the tokens that follow it on
+          // the row's path (counted only in pairs that reach the draft region,
+          // the same for the whole wave)
+          const bool drafts = TREE && key1 + kBlk > l_ctx;
+          auto distance = [&](int e) {
+            const int j = (e < 4 ? key0 : key1) + 4 * lg + (e & 3);
+            if (TREE && j >= l_ctx) return (int)__popcll((tm_r >> min(j - l_ctx, 63)) >> 1);
+            return position() - j;
+          };
           if (p.slopes) {
-            // less slope times the distance: in the context the positions'
-            // difference, for a tree's draft key the tokens that follow it on
-            // the row's path
+            // (scores that were not capped are scaled here)
+            const float by = p.cap_in > 0.f ? 1.f : p.sl2;
+            if (drafts) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int j = (e < 4 ? key0 : key1) + 4 * lg + (e & 3);
-              int dist = pos - j;
-              if constexpr (TREE)
-                if (j >= l_ctx) dist = __popcll((tmask >> (min(j - l_ctx, 63))) >> 1);
-              x[e] = fmaf(-slope, (float)dist, x[e]);
+              for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], by, -sl_r * (float)distance(e));
+            } else {
+              // -slope (pos - key - 4 lg - r) of both blocks' first keys, plus r slopes
+              const int far = position() - 4 * lg;
+              const float at0 = -sl_r * (float)(far - key0), at1 = -sl_r * (float)(far - key1);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], by, fmaf((float)(e & 3), sl_r, e < 4 ? at0 : at1));
             }
           }
           // keys that have left the row's window: only among the first of the
@@ -1325,13 +1330,8 @@ __global__ __launch_bounds__(kThreads, 1) void verify_attn_kernel(ParamsOf<SCORE
           // the context
           if (p.window && key0 < l_ctx + seq_c(s) - p.window) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int j = (e < 4 ? key0 : key1) + 4 * lg + (e & 3);
-              int dist = pos - j;
-              if constexpr (TREE)
-                if (j >= l_ctx) dist = __popcll((tmask >> (min(j - l_ctx, 63))) >> 1);
-              if (dist >= p.window) x[e] = -INFINITY;
-            }
+            for (int e = 0; e < 8; ++e)
+              if (distance(e) >= p.window) x[e] = -INFINITY;
           }
 #pragma unroll
           for (int e = 0; e < 8; ++e) sa[e >> 2][e & 3] = x[e];
@@ -1360,14 +1360,14 @@ __global__ __launch_bounds__(kThreads, 1) void verify_attn_kernel(ParamsOf<SCORE
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
                 const int k = (h == 0 ? key0 : key1) + 4 * lg + r - l_ctx;
-                if (k >= 0 && !((tmask >> (k & 63)) & 1u)) x[4 * h + r] = -INFINITY;
+                if (k >= 0 && !(((SCORED ? tm_r : tmask) >> (k & 63)) & 1u)) x[4 * h + r] = -INFINITY;
                 mx = fmaxf(mx, x[4 * h + r]);
               }
             }
           }
         }
         // (the scale is positive: max of the scaled scores)
-        if constexpr (SCORED) mx = row_max(mx);
+        if constexpr (SCORED) mx = row_max(mx) * x_scale;
         else mx = row_max(mx) * p.sl2;
         // raise the running max only when the pair's max passes it by
         // more than kLazyMax; the four lanes of a row decide alike
@@ -1384,7 +1384,7 @@ __global__ __launch_bounds__(kThreads, 1) void verify_attn_kernel(ParamsOf<SCORE
         float pr[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-          if constexpr (SCORED) pr[r] = __builtin_amdgcn_exp2f(x[r] - m_use);
+          if constexpr (SCORED) pr[r] = __builtin_amdgcn_exp2f(fmaf(x[r], x_scale, -m_use));
           else pr[r] = __builtin_amdgcn_exp2f(fmaf(x[r], p.sl2, -m_use));
           l_lane += pr[r];
         }
@@ -1718,12 +1718,6 @@ __global__ __launch_bounds__(kThreads, 1) void verify_attn_kernel(ParamsOf<SCORE
       merge_units<D, THROUGH, OUT>(p, seqs, ctid, sh_share[f0 ? f0 - 1 : 0], sh_share[f1 ? f1 - 1 : 0], f0 != 0, f1 != 0);
   }
   report_give_up(gave_up);
-}
-
-// Zero the per-unit counters of a workspace.
-__global__ void zero_counters_kernel(int* counters, int n) {
-  const int i = blockIdx.x * blockDim.x + threadIdx.x;
-  if (i < n) counters[i] = 0;
 }
 
 // ---------------------------------------------------------------- host side
