@@ -24,7 +24,7 @@
 //   * with a small top_k only the best tokens matter: a histogram of the
 //     threads' maxima gives a bin edge that at least k tokens pass, and those
 //     alone are listed and weighed.
-// One workgroup of 8 waves per row holds the row in LDS when it fits (two
+// One workgroup per row holds the row in LDS when it fits (two
 // rows of up to 62.5 KB per CU), so the logits are read from HBM once.
 #include <hip/hip_runtime.h>
 
@@ -41,8 +41,6 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kThreads = 512;
-constexpr int kWaves = kThreads / 64;
 constexpr int kList = 256;                 // tokens put in order at once
 constexpr int kBest = 128;                 // top_k for which about 150 tokens pass the 512 threads' maxima
 constexpr int kMaxVocab = 1 << 20;         // weights of 2^42 add up below 2^63
@@ -180,8 +178,9 @@ __device__ __forceinline__ double exp2_poly(double f) {
 }
 
 // One row's sampling, by all threads of a workgroup.
-template <bool BF16, int kRowLds>
+template <bool BF16, int kRowLds, int kThreads>
 struct Row {
+  static constexpr int kWaves = kThreads / 64;
   static constexpr int kElt = BF16 ? 2 : 4;
   static constexpr int kPer = 16 / kElt;             // logits per 16-byte vector
   static constexpr int kBins = BF16 ? 4096 : 2048;   // fp32 ones have a mass of 8 bytes each beside the count
@@ -282,30 +281,24 @@ struct Row {
     }
   }
 
-  // Weight in units, and the same before it was rounded.  Additions of 1.5 x
-  // 2^52 and 2^52 round to integers in the low bits of a double, and a power of
-  // two goes straight into the exponent: the conversions and ldexp take four
-  // times an addition's cycles.
-  __device__ __forceinline__ u64 weight(float x, double& exact) const {
+  // 2^(units - y) for y >= 0, at most 2^-18 from 2^-60 on and for NaN.  Additions
+  // of 1.5 x 2^52 and 2^52 (whole) round to integers in the low bits of a double,
+  // and a power of two goes straight into the exponent: the conversions and
+  // ldexp take four times an addition's cycles.
+  static __device__ __forceinline__ double power(double y, int units) {
     constexpr double kRound = 6755399441055744.0;
-    const double y = x == m ? 0.0 : (md - (double)x) * c;
-    const bool in = y < kMost;   // (false for NaN)
+    y = fmin(y, 60.0);
     const double t = y + kRound;
     const double q = exp2_poly((t - kRound) - y);
-    const int n = (int)(uint32_t)__double_as_longlong(t);   // (junk where !in)
-    exact = in ? __longlong_as_double((long long)((u64)__double_as_longlong(q) + ((u64)(kUnit - n) << 52))) : 0.0;
-    return whole(exact);
+    return __hiloint2double(__double2hiint(q) + ((units - __double2loint(t)) << 20), __double2loint(q));
   }
   static __device__ __forceinline__ u64 whole(double exact) {
     return (u64)__double_as_longlong(exact + 4503599627370496.0) & 0xfffffffffffffull;
   }
-  // 2^-y for y >= 0; 0 from 2^-43 on (and for NaN)
-  static __device__ __forceinline__ void ratio_of(double y, double& r) {
-    constexpr double kRound = 6755399441055744.0;
-    const double t = y + kRound;
-    const double q = exp2_poly((t - kRound) - y);
-    const int n = (int)(uint32_t)__double_as_longlong(t);
-    r = y < kMost ? __longlong_as_double((long long)((u64)__double_as_longlong(q) - ((u64)n << 52))) : 0.0;
+  // weight in units, and the same before it was rounded (finite maximum)
+  __device__ __forceinline__ u64 weight(float x, double& exact) const {
+    exact = power((md - (double)x) * c, kUnit);
+    return whole(exact);
   }
 
   // loads the row and returns its maximum, -inf for a row without any mass
@@ -647,7 +640,7 @@ struct Row {
 
   // log of a token's share of the kept mass
   __device__ __forceinline__ float log_share(float x, u64 kept) const {
-    const double d = x == m ? 0.0 : ((double)x - md) * (c * 0.69314718055994530942);
+    const double d = ((double)x - md) * (c * 0.69314718055994530942);
     return (float)(d - log((double)kept * (1.0 / (double)(1ull << kUnit))));
   }
 
@@ -717,6 +710,21 @@ struct Row {
     token = sh.found_index;
     logp = log_share(sh.found_logit, kept);
     return true;
+  }
+
+  // The token of a row with infinite logits: one of them, all weighing a unit.
+  __device__ __forceinline__ void draw_infinite(float u, int k, bool by_p, float top_p, int& token, float& logp) {
+    int mine = 0;
+    each([&](float x) { return x == m; }, [&](float, int) { ++mine; });
+    int nb, n;
+    u64 wb, wa;
+    scan(mine, 0, nb, wb, n, wa);
+    u64 kept = (u64)min(n, k) << kUnit;
+    if (by_p) kept = ((share_end(top_p, kept) >> kUnit) + 1) << kUnit;
+    find_nth(m, (int)(share_of(u, kept) >> kUnit));
+    __syncthreads();
+    token = sh.found_index;
+    logp = -(float)log((double)(kept >> kUnit));
   }
 
   // Counts (bf16) or weighs (fp32) every token into its bin.
@@ -790,7 +798,7 @@ struct Row {
             const int bin = bin_of(K);
             atomicAdd(&sh.hist.mass[bin], w[e]);
             if (by_k) atomicAdd(&sh.hist.count[bin], 1);
-            if (exact[e] >= cut) passes += w[e];
+            if (cut > 0.0 && exact[e] >= cut) passes += w[e];
           }
         }
       }
@@ -820,6 +828,11 @@ struct Row {
       __syncthreads();
       token = sh.found_index < INT_MAX ? sh.found_index : -1;
       logp = token < 0 ? -INFINITY : 0.f;
+      return;
+    }
+    if (m == INFINITY) {
+      // infinite logits share the mass
+      draw_infinite(u, by_k ? k : p.V, by_p, top_p, token, logp);
       return;
     }
     md = uniform((double)m);
@@ -862,7 +875,7 @@ struct Row {
       const int K0 = pattern_of(tid * kOwn), from = is_mid ? 0 : K0 - min(K0, top);
       double w0, ratio;
       weight(value_at(min(K0, top)), w0);
-      ratio_of(((double)value_at(K0 - (kOwn - 2)) - (double)value_at(K0 - (kOwn - 1))) * c, ratio);
+      ratio = power(((double)value_at(K0 - (kOwn - 2)) - (double)value_at(K0 - (kOwn - 1))) * c, 0);
 #pragma unroll
       for (int i = 0; i < kOwn; ++i) {
         const bool there = i >= from;   // (above the maximum there are only NaN)
@@ -1036,9 +1049,9 @@ __device__ __forceinline__ void accept(const Params& p, int b, int c, int lane) 
 
 // One workgroup per row.  (As many as fit the chip, each with every 512th row:
 // 2048 rows of 32000 took 107 us, not 94.)
-template <bool BF16, int kRowLds, bool ACCEPT>
-__global__ __launch_bounds__(kThreads, kRowLds == kRowSmall || kRowLds == kRowSmallF32 ? 4 : 2) void sample_kernel(Params p) {
-  using R = Row<BF16, kRowLds>;
+template <bool BF16, int kRowLds, int kThreads, bool ACCEPT>
+__global__ __launch_bounds__(kThreads, 4) void sample_kernel(Params p) {
+  using R = Row<BF16, kRowLds, kThreads>;
   __shared__ typename R::Shared sh;
   // MODE.IEEE off: a maximum with one NaN operand, signalling or quiet, is the
   // other operand
@@ -1094,12 +1107,18 @@ template <bool BF16, bool ACCEPT>
 void launch_rows(const Params& p, unsigned rows, hipStream_t s) {
   constexpr int kSmall = BF16 ? kRowSmall : kRowSmallF32;
   const int64_t bytes = ((int64_t)p.V * (BF16 ? 2 : 4) + 15) / 16 * 16;
-  if (bytes <= kSmall)
-    hipLaunchKernelGGL((sample_kernel<BF16, kSmall, ACCEPT>), dim3(rows), dim3(kThreads), 0, s, p);
+  // 16 waves to a row where it has a CU to itself: few rows, or long ones (16
+  // rows of 32000 bf16 17.9 -> 15.5 us, 256 of fp32 33.0 -> 30.1, 64 of 151936
+  // bf16 66 -> 46); where two rows share one, 8 waves each, with the registers
+  // that a row's work takes.
+  if (bytes <= kSmall && rows > kCUs)
+    hipLaunchKernelGGL((sample_kernel<BF16, kSmall, 512, ACCEPT>), dim3(rows), dim3(512), 0, s, p);
+  else if (bytes <= kSmall)
+    hipLaunchKernelGGL((sample_kernel<BF16, kSmall, 1024, ACCEPT>), dim3(rows), dim3(1024), 0, s, p);
   else if (bytes <= kRowLarge)
-    hipLaunchKernelGGL((sample_kernel<BF16, kRowLarge, ACCEPT>), dim3(rows), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((sample_kernel<BF16, kRowLarge, 1024, ACCEPT>), dim3(rows), dim3(1024), 0, s, p);
   else
-    hipLaunchKernelGGL((sample_kernel<BF16, 0, ACCEPT>), dim3(rows), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((sample_kernel<BF16, 0, 1024, ACCEPT>), dim3(rows), dim3(1024), 0, s, p);
 }
 
 template <bool ACCEPT>

@@ -947,7 +947,10 @@ __global__ __launch_bounds__(kThreads, 1) void verify_attn_kernel(ParamsOf<SCORE
   // merge of the waves' partial states at every unit end costs more than the
   // compute that two more waves per block would take over), four waves idle.
   // From three blocks on (n_rbp = 8), a wave computes its block's whole
-  // tile, which is cheaper than merging at the end of every unit.
+  // tile, which is cheaper than merging at the end of every unit; but in
+  // scored calls, which compute longer, three and four blocks take two waves
+  // each (64 sequences, 16-token trees, four row blocks: capped 92 -> 86 us,
+  // with slopes 91 -> 85; from five blocks on no waves are left).
   int R = 0, n_rbp = 1, nks = 1, rb = 0, kslot = 0, l_ctx = 0, row = 0, tok = 0, vis = 0;
   bool active = false, row_valid = false;
   uint64_t tmask = 0;   // (tree drafts) this lane's row: bit k = sees draft key l_ctx + k
@@ -963,7 +966,7 @@ __global__ __launch_bounds__(kThreads, 1) void verify_attn_kernel(ParamsOf<SCORE
   // there, as (x + 1/2) / g lies at least 1 / (2 g) from an integer
   const float inv_g = 1.f / (float)g;
   auto div_g = [&](int x) { return (int)(((float)x + 0.5f) * inv_g); };
-  auto rbp_shift = [&](int n_rb) { return n_rb <= 1 ? 0 : n_rb <= 2 ? 1 : 3; };   // log2 n_rbp
+  auto rbp_shift = [&](int n_rb) { return n_rb <= 1 ? 0 : n_rb <= 2 ? 1 : SCORED && n_rb <= 4 ? 2 : 3; };   // log2 n_rbp
   // waves that share a row block's tiles (key slots)
   auto key_slots = [&](int n_rb, int sh) { return n_rb == 2 ? 2 : min(kConsumers >> sh, C::kNKB / 2); };
   auto roles = [&](const Cursor& cu) {
