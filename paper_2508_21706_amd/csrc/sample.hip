@@ -461,15 +461,19 @@ struct Row {
   // The place of list entry tid / g among the n listed: the entries and the
   // mass before it.  g threads share an entry's comparisons, so that each has
   // few and their sums few steps.
-  __device__ __forceinline__ int groups(int n) const { return n <= 16 ? 1 : 2; }   // (n <= kList)
-  static_assert(2 * kList <= kThreads, "a thread or two per entry");
+  __device__ __forceinline__ int groups(int n) const {   // (n <= kList)
+    int g = kThreads / kList;
+    while (g < 8 && 2 * g * n <= kThreads) g *= 2;
+    return g;
+  }
   __device__ __forceinline__ void place(int n, int g, int& rank, u64& before) const {
-    const int e = tid / g;
+    const int e = tid >> __builtin_ctz(g);
     rank = 0;
     before = 0;
     if (e < n) {
       const u64 own = sh.list[e].order;
-      for (int f = tid % g; f < n; f += g) {
+#pragma unroll 4
+      for (int f = tid & (g - 1); f < n; f += g) {
         const Entry o = sh.list[f];
         if (o.order > own) {
           ++rank;
@@ -546,8 +550,8 @@ struct Row {
       int rank;
       u64 inside;
       place(n, g, rank, inside);
-      const int e = tid / g;
-      if (e < n && tid % g == 0) {
+      const int e = tid >> __builtin_ctz(g);
+      if (e < n && (tid & (g - 1)) == 0) {
         const Entry own = sh.list[e];
         const u64 at = by_count ? (u64)rank : inside;
         if (left >= at && left - at < (by_count ? 1 : own.weight)) {
@@ -676,8 +680,8 @@ struct Row {
     int rank;
     u64 before;
     place(n, g, rank, before);
-    const int e = tid / g;
-    const bool owner = e < n && tid % g == 0;
+    const int e = tid >> __builtin_ctz(g);
+    const bool owner = e < n && (tid & (g - 1)) == 0;
     Entry own_entry = {0, 0};
     if (owner) own_entry = sh.list[e];
     const u64 weight_e = own_entry.weight;
