@@ -567,16 +567,19 @@ def _ptr(t: Optional[torch.Tensor]):
 def _token_stride(t: torch.Tensor, name: str, shape, dtype, gpu: int) -> int:
     """Elements from one token's row of ``t`` [B, C_max, H, D] to the next's;
     a row's heads lie side by side."""
-    if t.shape != shape or t.dtype is not dtype or gpu < 0 or t.get_device() != gpu:
+    if t.shape != shape or t.dtype is not dtype:
         _check_on(t.contiguous(), name, shape, dtype, gpu)
     B, C, H, D = shape
     sb, sc, sh, sd = t.stride()
-    if sc == H * D and sd == 1 and sh == D and sb == C * sc:
-        return sc
-    stride = sc if C > 1 else sb if B > 1 else H * D
-    if (D > 1 and sd != 1) or (H > 1 and sh != D) or (B > 1 and C > 1 and sb != C * sc):
-        raise ValueError(f"{name} must be rows of side-by-side heads at one distance from token to token")
-    return stride
+    if sc != H * D or sd != 1 or sh != D or sb != C * sc:
+        # (one row for all tokens, as expand() makes, is at a distance of 0)
+        if (D > 1 and sd != 1) or (H > 1 and sh != D) or (B > 1 and C > 1 and sb != C * sc) or \
+                (C > 1 and sc == 0) or (B > 1 and sb == 0):
+            raise ValueError(f"{name} must be rows of side-by-side heads at one distance from token to token")
+        sc = sc if C > 1 else sb if B > 1 else H * D
+    if gpu < 0 or t.get_device() != gpu:
+        _check_on(t.contiguous(), name, shape, dtype, gpu)
+    return sc
 
 
 def append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor,
@@ -757,11 +760,13 @@ def sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature: Optional[t
         raise ValueError("logits must be [N, V]")
     N, V = logits.shape
     dev = logits.get_device()
-    if dev < 0:
-        raise ValueError("logits must be a GPU tensor")
     if V > 1 and logits.stride(1) != 1:
         raise ValueError("the entries of a row of logits must lie side by side")
     stride = logits.stride(0) if N > 1 else V
+    if stride == 0 and V > 0:   # (one row for all, as expand() makes: a stride of 0 is the library's word for V)
+        raise ValueError("every row of logits must have memory of its own")
+    if dev < 0:
+        raise ValueError("logits must be a GPU tensor")
     _check_on(uniforms, "uniforms", (N,), torch.float32, dev)
     settings = _sampling(N, dev, temperature, top_k, top_p, min_p)
     if out is None:

@@ -208,3 +208,15 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         pkg.sample(torch.zeros((8,)), torch.zeros((2,)))
     with pytest.raises(ValueError, match="GPU"):
         pkg.accept_sample(torch.zeros((1, 2, 8)), torch.zeros((1, 2), dtype=torch.int32), lens, lens, torch.zeros((1, 2)))
+
+
+def test_binding_refuses_rows_without_memory_of_their_own():
+    """(expand() gives such rows a stride of 0, which the descriptors take for
+    side-by-side rows)"""
+    for B, C, row in ((1, 3, (1, 1, 2, 64)), (2, 1, (1, 1, 2, 64)), (2, 3, (1, 1, 2, 64)), (2, 3, (2, 1, 2, 64)),
+                      (2, 3, (1, 3, 2, 64))):
+        with pytest.raises(ValueError, match="one distance"):
+            bd._token_stride(torch.zeros(row).expand(B, C, 2, 64), "k", (B, C, 2, 64), torch.float32, -1)
+    for V in (1, 8):
+        with pytest.raises(ValueError, match="memory of its own"):
+            pkg.sample(torch.zeros((1, V)).expand(3, V), torch.zeros((3,)))
