@@ -76,7 +76,8 @@ enum {
                                      in [0, D], rope_style is not a specmoe_rope_style,
                                      or norm_eps is negative or not finite           */
   SPECMOE_ERR_SCORE = -17         /* (specmoe_verify_attn_scored) softcap or window is
-                                     negative, or softcap is not finite              */
+                                     negative, or softcap or scale / softcap is not
+                                     finite                                          */
 };
 
 /* desc->flags bits. */
@@ -302,7 +303,7 @@ typedef struct specmoe_score {
  *                specmoe_verify_attn_paged, or both NULL for a contiguous
  *                cache; draft_mask as in specmoe_verify_attn_tree, or NULL.
  *   out          device, 16-byte aligned: [B, C_max, Hq, D] of desc's dtype
- *                (the type that the projection after it takes).
+ *                (the type that the projection after it takes); not q's memory.
  *   score        host pointer to the settings; any of them may be off.
  *
  * A token that sees no key gets out = 0 and lse = -inf, as padding rows do.

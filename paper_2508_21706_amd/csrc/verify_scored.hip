@@ -34,6 +34,7 @@ extern "C" int specmoe_verify_attn_scored(const void* q, const void* k_cache, co
   if ((reinterpret_cast<uintptr_t>(score->slopes) | reinterpret_cast<uintptr_t>(score->starts)) & 3u)
     return SPECMOE_ERR_ALIGN;
   p.cap_in = score->softcap > 0.f ? scale / score->softcap : 0.f;
+  if (!isfinite(p.cap_in)) return SPECMOE_ERR_SCORE;
   p.cap2 = score->softcap * kLog2e;
   p.slopes = score->slopes;
   p.starts = score->starts;

@@ -193,6 +193,12 @@ def test_scored_refusals(lib):
     assert scored(lib, desc(B=0), q=None, out=None) == 0
 
 
+def test_scored_refuses_a_cap_too_small_for_its_scale(lib):
+    d = bd.make_desc(2, 32, 8, 128, 5, 2304, 1)
+    d.workspace, d.workspace_bytes = FAKE, 1 << 30
+    assert scored(lib, d, bd.Score(1e-40, 0, None, None), scale=1.0) == -17     # (scale / softcap is infinite)
+
+
 def test_binding_refuses_host_tensors_and_wrong_shapes():
     k = torch.zeros((1, 2, 2, 64))
     lens = torch.zeros((1,), dtype=torch.int32)
