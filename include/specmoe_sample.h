@@ -78,7 +78,7 @@ typedef struct specmoe_sample_desc {
  * The caller owns every buffer; nothing is allocated, nothing synchronises
  * with the host, no workspace is needed, and calls may overlap.  All host
  * checks run before any HIP call: SPECMOE_ERR_NULL_POINTER (desc),
- * SPECMOE_ERR_DTYPE, SPECMOE_ERR_FLAGS, SPECMOE_ERR_SHAPE (N < 0 or > 2^22, V,
+ * SPECMOE_ERR_DTYPE, SPECMOE_ERR_FLAGS, SPECMOE_ERR_SHAPE (N < 0 or >= 2^22, V,
  * stride); then, with N > 0, SPECMOE_ERR_NULL_POINTER, SPECMOE_ERR_ALIGN, and
  * from HIP SPECMOE_ERR_LAUNCH.
  */
@@ -106,7 +106,7 @@ int specmoe_sample(const void* logits, const float* uniforms, const specmoe_samp
  * Every other argument, the workspace (one can serve both, and its size and
  * initialisation are those of specmoe_accept_greedy; desc->split is ignored),
  * ownership and the errors are those of specmoe_accept_greedy; in addition
- * V <= 2^20 (SPECMOE_ERR_SHAPE).
+ * V <= 2^20 and B C_max < 2^22 (SPECMOE_ERR_SHAPE).
  */
 int specmoe_accept_sample(const void* logits, const int32_t* tokens, const int32_t* ctx_lens,
                           const int32_t* chunk_lens, const float* uniforms, const specmoe_sampling* sampling,

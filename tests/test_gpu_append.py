@@ -207,3 +207,18 @@ def test_another_stream_and_empty_batch():
     none = torch.empty((0,), dtype=torch.int32, device=d)
     out = pkg.append_kv(x["q"][:0], x["k"][:0], x["v"][:0], x["k_cache"][:0], x["v_cache"][:0], none, none, inv_freq=inv)
     assert out.shape == (0, 3, 4, 64)
+
+
+def test_positions_past_two_to_the_thirty():
+    """A table of 2^31 - 65536 positions over two pages.  (The angle's own three
+    roundings, 2^-53 of 2^30 each, are six of the half-steps that the norm
+    would take.)"""
+    d = dev()
+    page, pos = 1 << 16, (1 << 30) + 3 * (1 << 16) + 77
+    table = torch.zeros((1, (1 << 15) - 1), dtype=torch.int32, device=d)
+    table[0, pos // page] = 1
+    gen = torch.Generator().manual_seed(9)
+    rand = lambda *shape: torch.randn(shape, generator=gen).to(d)   # noqa: E731
+    x = dict(q=rand(1, 2, 2, 64), k=rand(1, 2, 1, 64), v=rand(1, 2, 1, 64), k_cache=rand(2, 1, page, 64),
+             v_cache=rand(2, 1, page, 64), q_out=rand(1, 2, 2, 64), table=table)
+    check(x, [pos], [2], 64, label="past 2^30")
