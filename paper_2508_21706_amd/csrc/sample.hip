@@ -357,8 +357,8 @@ struct Row {
   }
 
   // the bins of this row: from its maximum down to where weights vanish
-  __device__ __forceinline__ void lay_bins() {
-    const double end = md - (kMost + 0.01) / c;
+  __device__ __forceinline__ void lay_bins(double T) {
+    const double end = md - (kMost + 0.01) * 0.69314718055994530942 * T;
     const float least = end > -3.4028234663852886e38 ? (float)end : -3.4028234663852886e38f;   // (NaN: the least number)
     top = uniform((int)(key_of(m) >> kDrop));
     int bottom = min(uniform((int)(key_of(least) >> kDrop)), top);
@@ -712,7 +712,7 @@ struct Row {
     }
     __syncthreads();
     token = sh.found_index;
-    logp = log_share(sh.found_logit, kept);
+    if (wave == 0) logp = log_share(sh.found_logit, kept);
     return true;
   }
 
@@ -810,7 +810,7 @@ struct Row {
     }
   }
 
-  // The row's token and log-probability, in every thread.
+  // The row's token, in every thread, and its log-probability, in the first wave's.
   __device__ __forceinline__ void draw(float u, float T, int k, float top_p, float min_p, int& token, float& logp) {
     clear_hist();
     if (tid == 0) {
@@ -842,7 +842,7 @@ struct Row {
     md = uniform((double)m);
     c = uniform(1.4426950408889634074 / (double)T);
     cut = uniform(min_p > 0.f ? (double)fminf(min_p, 1.f) * (double)(1ull << kUnit) : 0.0);
-    lay_bins();
+    lay_bins(T);
     if (by_k && k <= kBest) {
       if (draw_best(u, k, by_p, top_p, mine, token, logp)) return;
       __syncthreads();
@@ -1004,7 +1004,7 @@ struct Row {
       }
     }
     token = sh.found_index;
-    logp = log_share(sh.found_logit, kept);
+    if (wave == 0) logp = log_share(sh.found_logit, kept);
   }
 };
 
@@ -1084,7 +1084,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_kernel(Params p) {
   const int k = p.top_k ? p.top_k[b] : 0;
   const float top_p = p.top_p ? p.top_p[b] : 1.f, min_p = p.min_p ? p.min_p[b] : 0.f;
   int token;
-  float logp;
+  float logp = 0.f;
   R row(p, sh, p.logits + (size_t)n * p.stride);
   row.draw(u, T, k, top_p, min_p, token, logp);
   if constexpr (!ACCEPT) {
