@@ -37,11 +37,12 @@ METRIC = "effective KV HBM GB/s and verified draft tokens/sec, Mixtral shape B=6
 HBM_PEAK_GBS = 8000.0
 MFMA_BF16_PEAK_TFLOPS = 2500.0   # dense bf16 / f16 matrix-core peak of an MI355X
 MAIN_KERNEL = "verify_attn_kernel"
-KERNEL_SOURCE = os.path.join(ROOT, "paper_2508_21706_amd", "csrc", "verify_attn.hip")
+KERNEL_SOURCE = os.path.join(ROOT, "paper_2508_21706_amd", "csrc", "verify_kernel.h")
 SCHEDULE_SOURCE = os.path.join(ROOT, "paper_2508_21706_amd", "csrc", "schedule.h")
 ACCEPT_METRIC = "acceptance step: logits HBM GB/s and accepted-token decisions per second"
 ACCEPT_KERNEL = "accept_kernel"
 ACCEPT_SOURCE = os.path.join(ROOT, "paper_2508_21706_amd", "csrc", "accept.hip")
+ACCEPT_PLAN_SOURCE = os.path.join(ROOT, "paper_2508_21706_amd", "csrc", "accept_plan.h")
 
 
 def log(msg):
@@ -49,9 +50,9 @@ def log(msg):
 
 
 def source_digest(path: str = KERNEL_SOURCE) -> str:
-    """Of a kernel's source; of the attention kernel's with its schedule."""
+    """Of a kernel's source with its schedule (attention) or launch plan (acceptance)."""
     digest = hashlib.sha256()
-    for part in (path, SCHEDULE_SOURCE) if path == KERNEL_SOURCE else (path,):
+    for part in (path, SCHEDULE_SOURCE if path == KERNEL_SOURCE else ACCEPT_PLAN_SOURCE):
         with open(part, "rb") as f:
             digest.update(f.read())
     return digest.hexdigest()[:16]
