@@ -20,18 +20,19 @@
 //     order by comparing all with all;
 //   * bins cover the numbers from the maximum to where weights vanish.  Where
 //     those have too many patterns, the ones nearest to 0 (there are patterns
-//     without end, but hardly a token) share one bin that is searched by list;
+//     without end, but hardly a token) share one bin that is searched by list.
+//     bf16 logits below 64, as nearly all are, need no maximum for that: one
+//     layout of bins does for them, and a row is counted while it is loaded;
 //   * with a small top_k only the best tokens matter: a histogram of the
 //     threads' maxima gives a bin edge that at least k tokens pass, and those
 //     alone are listed and weighed.
 // One workgroup per row holds the row in LDS when it fits (two rows of up to
 // 62.5 KB per CU), so the logits are read from HBM once.  2048 bf16 rows of
-// 32000 tokens (131 MB, 26 us at a copy's rate) take 80 us with everything
-// kept, 45 with top-50 and 30 greedily: a row's load, histogram, scan and
-// search follow each other, and of the two rows on a CU rarely both compute,
-// so the vector units are busy for 43% of the time and HBM for a third.  64
-// fp32 rows take 29 us (the fp64 weights of a row on one CU), a bf16 row with
-// every setting on 8.4.
+// 32000 tokens (131 MB, 26 us at a copy's rate) take 68 us with everything
+// kept, 46 with top-50 and 30 greedily: what a row does after its load, 1000
+// instructions per wave and a dozen barriers, is not hidden by the one other
+// row on its CU.  64 fp32 rows take 29 us (the fp64 weights of a row on one
+// CU), one bf16 row with every setting on 8.
 #include <hip/hip_runtime.h>
 
 #include <limits.h>
@@ -325,10 +326,102 @@ struct Row {
       }
     }
     mine = hi;
+    return row_max(hi);
+  }
+  __device__ __forceinline__ float row_max(float hi) {
     hi = wave_max(hi);
     if (lane == 0) sh.part_max[wave] = hi;
     __syncthreads();
     return wave_max(sh.part_max[lane & (kWaves - 1)]);
+  }
+
+  // (bf16) The bins of most rows, laid before the maximum is known: all
+  // patterns of kAround <= |x| < 64, those nearer to 0 in one group.
+  static constexpr int kUsualBase = 0xc27f, kUsualMid = kBins / 2 - kOwn;   // (just below 64)
+  static constexpr int kAround = kUsualBase + 1 - kZero - kUsualMid;        // (a pattern: 2^-10)
+  static constexpr int kUsualSkip = kUsualBase + 1 - kZero + kAround - kOwn;
+  static constexpr int kUsualReach = kUsualSkip + kOwn + kBins / 2 - 1;
+  static constexpr int kNearShift = kRowLds ? 0 : 2;   // vectors of a thread per bit, as a power of two: up to 128 of them
+  static_assert(!BF16 || ((kMaxVocab / 8 / kThreads) >> kNearShift) <= 32 || kRowLds > 0, "a bit for each");
+
+  // (bf16) Loads the row and counts its tokens into those bins.  Returns the
+  // largest pattern, and in `near` which of the thread's vectors hold tokens
+  // around 0.  (load() and fill() one after the other took 12 instructions per
+  // token, not 8, and nothing overlapped the loads: 2048 rows of 32000, 80 us
+  // with everything kept and 79 with top-p 0.9, now 68 and 68.)
+  __device__ __forceinline__ int load_counting(uint32_t& near) {
+    typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+    typedef __attribute__((ext_vector_type(2))) short i16x2;
+    auto both = [](int x) { return u16x2{(unsigned short)x, (unsigned short)x}; };
+    // what lies outside the bins, NaN among it, counts in a spare one of its lane
+    const u16x2 out2 = both(kUsualReach + 1 + lane);
+    char* const counts = reinterpret_cast<char*>(sh.hist.count);
+    constexpr int kBatch = 4;   // 16-byte loads per lane in flight, while as many are counted
+    u32x4 next[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (tid + u * kThreads < nvec) next[u] = fetch(tid + u * kThreads);
+    __syncthreads();   // the bins are clear
+    u16x2 best = both(0);
+    near = 0;
+    int j = 0;
+    for (int v0 = tid; v0 < nvec; v0 += kBatch * kThreads) {
+      u32x4 x[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) x[u] = next[u];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        if (v0 + (kBatch + u) * kThreads < nvec) next[u] = fetch(v0 + (kBatch + u) * kThreads);
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u, ++j) {
+        if (v0 + u * kThreads >= nvec) continue;
+        if constexpr (kRowLds > 0) *reinterpret_cast<u32x4*>(sh.row + (size_t)(v0 + u * kThreads) * 16) = x[u];
+        u16x2 least = both(0x7fff);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t word = x[u][w];
+          const uint32_t sign = __builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2, word) >> (short)15);
+          const u16x2 K = __builtin_bit_cast(u16x2, word ^ (sign | 0x80008000u));
+          best = __builtin_elementwise_max(best, K);
+          least = __builtin_elementwise_min(least, __builtin_bit_cast(u16x2, word & 0x7fff7fffu));
+          const u16x2 d = __builtin_elementwise_min((u16x2)(both(kUsualBase) - K), out2);
+          const u16x2 bin = (u16x2)(__builtin_elementwise_min(d, both(kUsualMid)) +
+                                    __builtin_elementwise_sub_sat(d, both(kUsualSkip))) << (unsigned short)2;
+          atomicAdd(reinterpret_cast<int*>(counts + bin[0]), 1);
+          atomicAdd(reinterpret_cast<int*>(counts + bin[1]), 1);
+        }
+        if (least[0] < kAround || least[1] < kAround) near |= 1u << (j >> kNearShift);
+      }
+    }
+    const int hi = wave_max((int)max(best[0], best[1]));
+    if (lane == 0) sh.part_count[wave] = hi;
+    __syncthreads();
+    return uniform(wave_max(sh.part_count[lane & (kWaves - 1)]));
+  }
+  // The masses of the tokens around 0 in the vectors that `near` names.
+  __device__ __forceinline__ void weigh_near(uint32_t near) {
+    if (!near) return;
+    u64 sum = 0, above = 0;
+    for (; near; near &= near - 1) {
+      const int j0 = __builtin_ctz(near) << kNearShift;
+#pragma unroll 1
+      for (int j = j0; j < j0 + (1 << kNearShift); ++j) {
+        const int v = tid + j * kThreads;
+        if (v >= nvec) break;
+        const u32x4 x = vec(v);
+        uint32_t found = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) found |= ((x[e >> 1] >> (16 * (e & 1))) & 0x7fffu) < (uint32_t)kAround ? 1u << e : 0u;
+        for (; found; found &= found - 1) {
+          double exact;
+          const u64 w = weight(logit_at(v * kPer + __builtin_ctz(found)), exact);
+          sum += w;
+          above += exact >= cut ? w : 0;
+        }
+      }
+    }
+    atomicAdd(&sh.middle, sum);
+    if (cut > 0.0) atomicAdd(&sh.middle_above, above);
   }
 
   // sums over the workgroup of what the threads before hold, and the total
@@ -362,9 +455,12 @@ struct Row {
     }
   }
 
+  // below it, weights vanish
+  __device__ __forceinline__ double least_weighed(double T) const { return md - (kMost + 0.01) * 0.69314718055994530942 * T; }
+
   // the bins of this row: from its maximum down to where weights vanish
   __device__ __forceinline__ void lay_bins(double T) {
-    const double end = md - (kMost + 0.01) * 0.69314718055994530942 * T;
+    const double end = least_weighed(T);
     const float least = end > -3.4028234663852886e38 ? (float)end : -3.4028234663852886e38f;   // (NaN: the least number)
     top = uniform((int)(key_of(m) >> kDrop));
     int bottom = min(uniform((int)(key_of(least) >> kDrop)), top);
@@ -589,10 +685,14 @@ struct Row {
            [&](float x, int) {
              double exact;
              const u64 w = weight(x, exact);
-             const uint32_t part = (hi - key_of(x)) >> shift;
-             if (w) {
-               atomicAdd(&mass[part], w);
-               atomicAdd(&count[part], 1);
+             const uint32_t key = key_of(x), part = (hi - key) >> shift;
+             // lanes with the first one's key (rows of zeros) add together
+             const bool same = key == (uint32_t)uniform((int)key);
+             const u64 who = __ballot(same);
+             const int n = same ? __popcll(who) : 1;
+             if (!same || lane == __builtin_ctzll(who)) {
+               if (w) atomicAdd(&mass[part], w * (u64)n);
+               atomicAdd(&count[part], n);   // (a count goes over tokens without weight, too)
              }
            });
       __syncthreads();
@@ -753,6 +853,7 @@ struct Row {
       const u16x2 base2 = both(base), out2 = both(reach + 1), most2 = both(most), skip2 = both(skip),
                   reach2 = both(reach), spare2 = both(kBins + lane - last), mid2 = both(mid), group2 = both(~(kOwn - 1));
       char* const counts = reinterpret_cast<char*>(sh.hist.count);
+      u64 around = 0, around_above = 0;
       u32x4 next = vec(min(tid, nvec - 1));   // (read ahead of the additions, which LDS serves in order)
       for (int v = tid; v < nvec; v += kThreads) {
         const u32x4 x = next;
@@ -784,11 +885,15 @@ struct Row {
             if ((uint32_t)(base - K) <= (uint32_t)reach && in_middle(bin_of(K))) {
               double exact;
               const u64 u = weight(y, exact);
-              atomicAdd(&sh.middle, u);
-              if (exact >= cut) atomicAdd(&sh.middle_above, u);
+              around += u;
+              around_above += exact >= cut ? u : 0;
             }
           }
         }
+      }
+      if (around) {
+        atomicAdd(&sh.middle, around);
+        if (cut > 0.0) atomicAdd(&sh.middle_above, around_above);
       }
     } else {
       // (a vector's weights side by side: one after the other, each waits for
@@ -825,9 +930,31 @@ struct Row {
       sh.above = 0;
       sh.found_index = INT_MAX;
     }
-    float mine;
-    m = load(mine);
     const bool by_k = k > 0 && k < p.V, by_p = top_p < 1.f;   // (NaN: off)
+    float mine = 0.f;
+    uint32_t near = 0;
+    // most rows whose tokens all have to be weighed are counted as they are
+    // loaded, into the usual bins (those with a maximum of 64 or more, or NaN of
+    // that sign, or weight below the bins, once more below)
+    const bool all = BF16 && T > 0.f && k != 1 && !(by_k && k <= kBest) && !(by_p && !(top_p > 0.f));
+    bool usual = false;
+    if (all) {
+      top = load_counting(near);
+      usual = top <= kUsualBase;
+      if (usual) {
+        m = top < 0x7f ? -INFINITY : value_at(top);   // (below -inf's pattern: NaN)
+      } else {
+        float hi = -INFINITY;
+        for (int v = tid; v < nvec; v += kThreads) {
+          const u32x4 x = vec(v);
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) hi = fmaxf(hi, entry(x, e));
+        }
+        m = row_max(hi);
+      }
+    } else {
+      m = load(mine);
+    }
     if (!(T > 0.f) || k == 1 || (by_p && !(top_p > 0.f)) || m == -INFINITY) {
       // the first maximum; of a row without mass only greedily, and of one of
       // NaN none
@@ -848,14 +975,24 @@ struct Row {
     md = uniform((double)m);
     c = uniform(1.4426950408889634074 / (double)T);
     cut = uniform(min_p > 0.f ? (double)fminf(min_p, 1.f) * (double)(1ull << kUnit) : 0.0);
-    lay_bins(T);
-    if (by_k && k <= kBest) {
-      if (draw_best(u, k, by_p, top_p, mine, token, logp)) return;
-      __syncthreads();
-      clear_hist();
-      __syncthreads();
+    if (usual) usual = least_weighed(T) >= (double)value_at(kUsualBase - kUsualReach);
+    if (usual) {
+      base = kUsualBase;
+      reach = kUsualReach;
+      mid = kUsualMid;
+      skip = kUsualSkip;
+      weigh_near(near);
+    } else {
+      lay_bins(T);
+      const bool best = by_k && k <= kBest;
+      if (best && draw_best(u, k, by_p, top_p, mine, token, logp)) return;
+      if (all || best) {
+        __syncthreads();
+        clear_hist();
+        __syncthreads();
+      }
+      fill(by_k);
     }
-    fill(by_k);
     __syncthreads();
     if constexpr (BF16) {
       // -0 counts as 0
@@ -1122,7 +1259,7 @@ void launch_rows(const Params& p, unsigned rows, hipStream_t s) {
   // bf16 66 -> 46); where two rows share one, 8 waves each, with the registers
   // that a row's work takes (2048 rows, everything kept: 80.4 us with 8 waves,
   // 80.3 with 16 of 64 registers, which spill, 106 with 4; with top-p 0.9
-  // 79.0, 82.2 and 107).
+  // 79.0, 82.2 and 107; before rows were counted as they are loaded).
   if (bytes <= kSmall && rows > kCUs)
     hipLaunchKernelGGL((sample_kernel<BF16, kSmall, 512, ACCEPT>), dim3(rows), dim3(512), 0, s, p);
   else if (bytes <= kSmall)

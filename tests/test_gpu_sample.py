@@ -316,3 +316,71 @@ def test_bins_around_zero_and_far_apart(dtype):
         for kw in ({}, dict(temperature=[30.0] * N), dict(temperature=[1e6] * N), dict(top_k=[700] * N, top_p=[0.8] * N),
                    dict(top_k=[60] * N), dict(min_p=[0.4] * N, temperature=[5.0] * N)):
             check_rows(x, u, **kw, label=f"{dtype} {name} {str(kw)[:24]}")
+
+
+@pytest.mark.parametrize("V", [2000, 32000, 80001])
+def test_tokens_around_zero(V):
+    """bf16 logits next to 0, which share one bin: many zeros, many distinct
+    numbers, with and without weight, and counts that end among them."""
+    gen = torch.Generator().manual_seed(V)
+    u = np.float32([0.03, 0.31, 0.62, 0.97])
+    tiny = (torch.rand((4, V), generator=gen) - 0.5) * 2.0 ** -10
+    zeros = torch.where(torch.rand((4, V), generator=gen) < 0.5, tiny, torch.tensor(0.0))
+    few = torch.randint(0, V, (4, 200), generator=gen)
+    for name, x in (("distinct", tiny), ("zeros", zeros), ("signed zeros", torch.copysign(torch.zeros(4, V), tiny))):
+        x = x.to(torch.bfloat16).to(dev())
+        check_rows(x, u, label=f"{name}")
+        check_rows(x, u, temperature=[2.0 ** -13, 2.0 ** -12, 2.0 ** -11, 1e-6], label=f"{name}, cold")
+        check_rows(x, u, top_k=[V // 2, 129, 400, V - 1], top_p=[0.9] * 4, label=f"{name}, top_k")
+        for top in (8.0, 40.0):   # a few tokens far above: those around 0 weigh e^-8 and nothing
+            y = x.clone().scatter_(1, few.to(dev()), (top - torch.arange(200) / 64.0).repeat(4, 1).bfloat16().to(dev()))
+            check_rows(y, u, label=f"{name}, {top}")
+            check_rows(y, u, top_k=[150, 199, 500, V - 1], label=f"{name}, {top}, top_k")
+            check_rows(y, u, top_k=[V // 2] * 4, top_p=[0.9] * 4, min_p=[0.01] * 4, label=f"{name}, {top}, all")
+            check_rows(y, u, temperature=[30.0] * 4, top_k=[0, 0, 900, V // 3], label=f"{name}, {top}, hot")
+
+
+@pytest.mark.parametrize("V", [900, 32000, 80001])
+def test_maxima_and_minima_at_the_ends_of_the_bins(V):
+    gen = torch.Generator().manual_seed(V + 1)
+    x = torch.randn((10, V), generator=gen)
+    u = torch.rand((10,), generator=gen).numpy()
+    at = torch.randint(0, V, (10,), generator=gen)
+    for r, top in enumerate([63.5, 63.75, 64.0, 100.0, 1e4]):
+        x[r] *= 8.0
+        x[r, at[r]] = top
+    x[5] -= 62.0          # around the lowest bins, below them, and far below
+    x[6] -= 90.0
+    x[7] -= 1e5
+    x[8] *= 30.0          # weights that reach below the lowest bins
+    x[9] = x[9] * 0.5 - 64.0
+    x = x.to(torch.bfloat16).to(dev())
+    for kw in ({}, dict(temperature=[4.0] * 10), dict(temperature=[60.0] * 10), dict(temperature=[0.05] * 10),
+               dict(top_k=[300] * 10), dict(top_k=[10] * 10), dict(top_p=[0.97] * 10, temperature=[2.5] * 10),
+               dict(min_p=[0.003] * 10, top_k=[500] * 10)):
+        check_rows(x, u, **kw, label=str(kw)[:30])
+
+
+def test_infinities_and_nan_in_bf16():
+    inf, nan = float("inf"), float("nan")
+    V = 700
+    x = torch.randn((12, V), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    x[0, 1:] = -inf
+    x[1, ::2] = -inf
+    x[2] = -inf
+    x[3] = nan
+    x[4, 5:600] = nan
+    x[5, 17] = inf
+    x[6, [3, 650]] = inf
+    x[7, :] = torch.finfo(torch.bfloat16).min
+    x[7, 30:33] = 2.0
+    x[8, ::3], x[8, 1] = -0.0, 0.0
+    x[8].clamp_(max=0.0)
+    bits = x.view(torch.int16)
+    bits[9, ::5], bits[9, 1::5] = -1, 0x7f81       # NaN of both signs, quiet and signalling
+    bits[10] = -1
+    bits[11, ::2], bits[11, 1::2] = -64, -128      # NaN with the sign, and -inf
+    u = np.float32([0.3, 0.6, 0.1, 0.1, 0.7, 0.5, 0.6, 0.9, 0.02, 0.4, 0.2, 0.8])
+    for kw in ({}, dict(top_k=[5] * 12), dict(top_k=[400] * 12), dict(top_p=[0.8] * 12), dict(min_p=[0.5] * 12),
+               dict(temperature=[3.0] * 12), dict(temperature=[inf] * 12), dict(temperature=[1e-38] * 12)):
+        check_rows(x.to(dev()), u, **kw, label=str(kw)[:30])
