@@ -384,3 +384,21 @@ def test_infinities_and_nan_in_bf16():
     for kw in ({}, dict(top_k=[5] * 12), dict(top_k=[400] * 12), dict(top_p=[0.8] * 12), dict(min_p=[0.5] * 12),
                dict(temperature=[3.0] * 12), dict(temperature=[inf] * 12), dict(temperature=[1e-38] * 12)):
         check_rows(x.to(dev()), u, **kw, label=str(kw)[:30])
+
+
+def test_offsets_past_32_bits():
+    """More than 2^32 bytes of logits: the rows around 2^32 and the last ones
+    are drawn as they are alone."""
+    N, V, d = 70000, 32000, dev()
+    logits = torch.empty((N, V), dtype=torch.bfloat16, device=d)
+    gen = torch.Generator(device=d).manual_seed(12)
+    for r in range(0, N, 10000):
+        logits[r:r + 10000].normal_(std=2.0, generator=gen)
+    u = torch.rand((N,), generator=gen, device=d)
+    top_p = torch.full((N,), 0.9, device=d)
+    token, logp = pkg.sample(logits, u, top_p=top_p)
+    torch.cuda.synchronize()
+    for r in (0, 33553, 67108, 67109, 69990):   # (2^31 and 2^32 bytes: rows 33554 and 67108)
+        t, l = pkg.sample(logits[r:r + 3].clone(), u[r:r + 3].clone(), top_p=top_p[:3])
+        assert torch.equal(t, token[r:r + 3]) and torch.equal(l, logp[r:r + 3])
+    check_rows(logits[-2:], u[-2:].cpu().numpy(), top_p=[0.9] * 2, label="past 2^32")

@@ -288,3 +288,32 @@ def test_nan_and_infinity_stay_in_their_sequence():
     x2["k"][0], x2["v"][0] = 0, 0
     out2, lse2 = call(x2, 10.0)
     assert torch.equal(out[1], out2[1]) and torch.equal(lse[1], lse2[1]) and torch.isfinite(out[1]).all()
+
+
+def test_offsets_past_32_bits():
+    """Caches of more than 2^32 bytes: the last sequence's rows, under a window
+    that skips most of them."""
+    d = dev()
+    B, Hkv, S, D = 3, 8, 1 << 20, 128
+    k = torch.zeros((B, Hkv, S, D), dtype=torch.bfloat16, device=d)
+    v = torch.zeros_like(k)
+    ctx, chunk = [40, 0, S - 3], [2, 2, 3]
+    x = make(16, "bf16", [40, 0, 500], chunk, Hq=8, Hkv=8, window=100, slopes=True)
+    x["ctx"] = ctx
+    for b in range(B):
+        n = [42, 2, 503][b]
+        for big, small in ((k, x["k"]), (v, x["v"])):
+            big[b, :, ctx[b] + chunk[b] - n:ctx[b] + chunk[b]] = torch.nan_to_num(small[b, :, :n].to(d))
+    t = lambda a: torch.tensor(a, dtype=torch.int32, device=d)   # noqa: E731
+    slopes = x["slopes"].to(d)
+    out, lse = pkg.verify_attn_scored(x["q"].to(d), k, v, t(ctx), t(chunk), x["scale"], softcap=20.0, slopes=slopes,
+                                      window=100, check_lengths=True)
+    near, near_l = pkg.verify_attn_scored(x["q"].to(d), torch.nan_to_num(x["k"]).to(d), torch.nan_to_num(x["v"]).to(d),
+                                          t([40, 0, 500]), t(chunk), x["scale"], softcap=20.0, slopes=slopes, window=100)
+    torch.cuda.synchronize()
+    # (the same keys at the same distances; other tiles, so other roundings of
+    # the probabilities to bf16, one step each at most)
+    assert torch.isfinite(out).all()
+    valid = torch.isfinite(near_l)
+    assert torch.equal(valid, torch.isfinite(lse)) and (lse - near_l)[valid].abs().max() <= 1e-5
+    assert (out - near).abs().float().max() <= 2.0 ** -7 * torch.nan_to_num(x["v"]).abs().max().float().item()
