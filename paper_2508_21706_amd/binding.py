@@ -727,6 +727,7 @@ def verify_attn_scored(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Te
             workspace = alloc_workspace(desc, q.device, stream)
         desc.workspace = workspace.data_ptr()
         desc.workspace_bytes = workspace.nbytes
+    window = max(min(window, (1 << 31) - 1), -1)   # (the field has 32 bits, and so has a length)
     score = Score(softcap, window, _ptr(slopes), _ptr(starts))
     _launch(dev, lib.specmoe_verify_attn_scored, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
             _ptr(block_table), ctx_lens.data_ptr(), chunk_lens.data_ptr(), _ptr(draft_mask), float(scale),

@@ -317,3 +317,14 @@ def test_offsets_past_32_bits():
     valid = torch.isfinite(near_l)
     assert torch.equal(valid, torch.isfinite(lse)) and (lse - near_l)[valid].abs().max() <= 1e-5
     assert (out - near).abs().float().max() <= 2.0 ** -7 * torch.nan_to_num(x["v"]).abs().max().float().item()
+
+
+def test_windows_past_32_bits_hide_nothing():
+    x = make(17, "f32", [90, 5], [3, 2])
+    want = call(x, 7.0)
+    for window in (93, (1 << 31) - 1, 1 << 31, (1 << 32) + 1, 1 << 40):
+        got = call(dict(x, window=window), 7.0)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    for window in (-1, -(1 << 32)):
+        with pytest.raises(pkg.SpecMoEError):
+            call(dict(x, window=window), 7.0)
