@@ -145,13 +145,28 @@ __device__ __forceinline__ int wave_prefix(int x) {
   x += dpp<0x143, 0xc>(0, x);
   return x;
 }
-__device__ __forceinline__ u64 lane_of(u64 x, int lane) {
-  return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 |
-         (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
-}
 template <int CTRL, int ROWS>
 __device__ __forceinline__ u64 dpp64(u64 x) {
   return (u64)(uint32_t)dpp<CTRL, ROWS>(0, (int)(x >> 32)) << 32 | (uint32_t)dpp<CTRL, ROWS>(0, (int)x);
+}
+template <class T>
+__device__ __forceinline__ T row_prefix(T x) {   // within each 16 lanes
+  if constexpr (sizeof(T) == 8) {
+    x += dpp64<0x111, 0xf>(x);
+    x += dpp64<0x112, 0xf>(x);
+    x += dpp64<0x114, 0xf>(x);
+    x += dpp64<0x118, 0xf>(x);
+  } else {
+    x += dpp<0x111, 0xf>(0, x);
+    x += dpp<0x112, 0xf>(0, x);
+    x += dpp<0x114, 0xf>(0, x);
+    x += dpp<0x118, 0xf>(0, x);
+  }
+  return x;
+}
+__device__ __forceinline__ u64 lane_of(u64 x, int lane) {
+  return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
 }
 __device__ __forceinline__ u64 wave_prefix(u64 x) {
   x += dpp64<0x111, 0xf>(x);
@@ -435,8 +450,9 @@ struct Row {
     }
     __syncthreads();
     // the waves' totals, one per lane, summed in the first lanes
-    const int np = wave_prefix(sh.part_count[lane & (kWaves - 1)]);
-    const u64 wp = wave_prefix(sh.part_mass[lane & (kWaves - 1)]);
+    static_assert(kWaves <= 16, "totals in one row of lanes");
+    const int np = row_prefix(sh.part_count[lane & (kWaves - 1)]);
+    const u64 wp = row_prefix(sh.part_mass[lane & (kWaves - 1)]);
     n_before = ni - n;
     w_before = wi - w;
     if (wave > 0) {
@@ -609,12 +625,13 @@ struct Row {
           hit |= (y - 0x00010001u) & ~y;
         }
       }
-      if (hit & 0x80008000u)
-        for (int e = 0; e < kPer; ++e) {
-          const int index = v * kPer + e;
-          if (index < p.V && logit_at(index) == value)
-            sh.indices[n > 1 ? atomicAdd(&sh.n_list, 1) & (kList - 1) : 0] = index;
-        }
+      if (hit & 0x80008000u) {
+        uint32_t found = 0;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) found |= entry(x, e) == value ? 1u << e : 0u;
+        for (; found; found &= found - 1)   // (value is finite: none beyond the row's end)
+          sh.indices[n > 1 ? atomicAdd(&sh.n_list, 1) & (kList - 1) : 0] = v * kPer + __builtin_ctz(found);
+      }
     }
   }
 
