@@ -290,15 +290,22 @@ struct Row {
   // found first, then taken one by one.
   template <class WANT, class F>
   __device__ __forceinline__ void each(WANT want, F f) const {
-    for (int v = tid; v < nvec; v += kThreads) {
-      const u32x4 x = vec(v);
-      uint32_t found = 0;
+    constexpr int kAhead = kRowLds ? 1 : 4;   // vectors read at once
+    for (int v0 = tid; v0 < nvec; v0 += kAhead * kThreads) {
+      u32x4 x[kAhead];
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) found |= want(entry(x, e)) ? 1u << e : 0u;
-      while (found) {
-        const int index = v * kPer + __builtin_ctz(found);
-        found &= found - 1;
-        if (index < p.V) f(logit_at(index), index);
+      for (int j = 0; j < kAhead; ++j) x[j] = vec(min(v0 + j * kThreads, nvec - 1));
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int v = v0 + j * kThreads;
+        uint32_t found = 0;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) found |= want(entry(x[j], e)) ? 1u << e : 0u;
+        while (found && v < nvec) {
+          const int index = v * kPer + __builtin_ctz(found);
+          found &= found - 1;
+          if (index < p.V) f(logit_at(index), index);
+        }
       }
     }
   }
@@ -326,7 +333,9 @@ struct Row {
   // loads the row and returns its maximum, -inf for a row without any mass
   __device__ __forceinline__ float load(float& mine) {
     float hi = -INFINITY;
-    constexpr int kBatch = 4;   // 16-byte loads per lane in flight
+    // 16-byte loads per lane in flight (rows that fit no LDS: one of 151936 fp32
+    // 16.0 -> 14.1 us greedily with 8, 64 of bf16 11.6 -> 12.4)
+    constexpr int kBatch = kRowLds || BF16 ? 4 : 8;
     for (int v0 = tid; v0 < nvec; v0 += kBatch * kThreads) {
       u32x4 x[kBatch];
 #pragma unroll
@@ -530,27 +539,31 @@ struct Row {
     __syncthreads();
     const float least = value_of(lo);
     constexpr int kSpan = 64 / kPer;   // vectors of a lane whose finds fit 64 bits
+    constexpr int kAhead = kRowLds ? 2 : 4;   // of them read at once
     for (int c0 = 0; c0 < nvec; c0 += kSpan * kThreads) {
       u64 found = 0;
-#pragma unroll 2
-      for (int j = 0; j < kSpan; ++j) {
-        const int v = c0 + j * kThreads + tid;
-        if (v >= nvec) break;
-        const u32x4 x = vec(v);
-        bool some = true;
-        if constexpr (TOP) {
-          float most = entry(x, 0);
+      for (int j0 = 0; j0 < kSpan; j0 += kAhead) {
+        u32x4 x[kAhead];
 #pragma unroll
-          for (int e = 1; e < kPer; ++e) most = fmaxf(most, entry(x, e));
-          some = most >= least;
-        }
-        if (some) {
-          uint32_t in = 0;
+        for (int j = 0; j < kAhead; ++j) x[j] = vec(min(c0 + (j0 + j) * kThreads + tid, nvec - 1));
 #pragma unroll
-          for (int e = 0; e < kPer; ++e)
-            in |= (TOP ? entry(x, e) >= least : key_of(entry(x, e)) - lo <= hi - lo) ? 1u << e : 0u;
-          found |= (u64)in << (kPer * j);
+        for (int j = 0; j < kAhead; ++j) {
+          bool some = c0 + (j0 + j) * kThreads + tid < nvec;
+          if constexpr (TOP) {
+            float most = entry(x[j], 0);
+#pragma unroll
+            for (int e = 1; e < kPer; ++e) most = fmaxf(most, entry(x[j], e));
+            some = some && most >= least;
+          }
+          if (some) {
+            uint32_t in = 0;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+              in |= (TOP ? entry(x[j], e) >= least : key_of(entry(x[j], e)) - lo <= hi - lo) ? 1u << e : 0u;
+            found |= (u64)in << (kPer * (j0 + j));
+          }
         }
+        if (c0 + (j0 + kAhead) * kThreads >= nvec) break;
       }
       // one place in the list per wave, then one per lane
       const int n = __popcll(found), upto = wave_prefix(n);
@@ -663,32 +676,15 @@ struct Row {
   // The token at position `left` (a count or a mass) among those with keys from
   // lo to hi, with mass `before` before them.
   __device__ __forceinline__ void search_keys(uint32_t lo, uint32_t hi, bool by_count, u64 left, u64 before) {
-    const int n = gather<false>(lo, hi);
-    if (n <= kList) {
-      const int g = groups(n);
-      int rank;
-      u64 inside;
-      place(n, g, rank, inside);
-      const int e = tid >> __builtin_ctz(g);
-      if (e < n && (tid & (g - 1)) == 0) {
-        const Entry own = sh.list[e];
-        const u64 at = by_count ? (u64)rank : inside;
-        if (left >= at && left - at < (by_count ? 1 : own.weight)) {
-          sh.found_index = (int)~(uint32_t)own.order;
-          sh.found_logit = value_of((uint32_t)(own.order >> 32));
-          sh.found_mass = before + inside + own.weight;
-        }
-      }
-      return;
-    }
-    // Many tokens (nearly equal logits, or a bin around 0): the keys are cut
-    // into ranges until one holds a single key, whose tokens are counted by
-    // index.  1024 ranges, of counts and masses in the list's place.
+    int n = gather<false>(lo, hi);
+    // Many tokens (nearly equal logits, a bin around 0, long rows): the keys are
+    // cut into ranges until one holds a list's or a single key's.  1024 ranges,
+    // of counts and masses in the list's place.
     constexpr int kParts = 1024, kHalves = kParts / kThreads;
     static_assert(sizeof(sh.hist) >= kParts * 12, "room for the ranges");
     int* const count = reinterpret_cast<int*>(&sh.hist);
     u64* const mass = reinterpret_cast<u64*>(count + kParts);
-    for (int level = 0; level < 4 && lo != hi; ++level) {   // (ten bits of the key each)
+    while (n > kList && lo != hi) {   // (ten bits of the key each time)
       const uint32_t span = hi - lo;
       const int shift = max(0, 32 - __builtin_clz(span) - 10);   // span >> shift < kParts
       __syncthreads();
@@ -706,10 +702,10 @@ struct Row {
              // lanes with the first one's key (rows of zeros) add together
              const bool same = key == (uint32_t)uniform((int)key);
              const u64 who = __ballot(same);
-             const int n = same ? __popcll(who) : 1;
+             const int times = same ? __popcll(who) : 1;
              if (!same || lane == __builtin_ctzll(who)) {
-               if (w) atomicAdd(&mass[part], w * (u64)n);
-               atomicAdd(&count[part], n);   // (a count goes over tokens without weight, too)
+               if (w) atomicAdd(&mass[part], w * (u64)times);
+               atomicAdd(&count[part], times);   // (a count goes over tokens without weight, too)
              }
            });
       __syncthreads();
@@ -732,17 +728,37 @@ struct Row {
           sh.bin = tid * kHalves + k;
           sh.before = wb;
           sh.count_before = nb;
+          sh.n = n_in[k];
         }
         nb += n_in[k];
         wb += w_in[k];
       }
       __syncthreads();
+      n = uniform(sh.n);
       before += sh.before;
       left -= by_count ? (u64)sh.count_before : sh.before;
       hi -= (uint32_t)sh.bin << shift;
       lo = max(lo, hi - ((1u << shift) - 1u));
+      if (n <= kList) n = gather<false>(lo, hi);
     }
-    // one key: its tokens weigh the same
+    if (n <= kList) {
+      const int g = groups(n);
+      int rank;
+      u64 inside;
+      place(n, g, rank, inside);
+      const int e = tid >> __builtin_ctz(g);
+      if (e < n && (tid & (g - 1)) == 0) {
+        const Entry own = sh.list[e];
+        const u64 at = by_count ? (u64)rank : inside;
+        if (left >= at && left - at < (by_count ? 1 : own.weight)) {
+          sh.found_index = (int)~(uint32_t)own.order;
+          sh.found_logit = value_of((uint32_t)(own.order >> 32));
+          sh.found_mass = before + inside + own.weight;
+        }
+      }
+      return;
+    }
+    // one key: its tokens weigh the same, and are counted by index
     const float value = value_of(lo);
     double exact;
     const u64 w = weight(value, exact);
@@ -916,8 +932,15 @@ struct Row {
       // (a vector's weights side by side: one after the other, each waits for
       // its own polynomial)
       u64 passes = 0;
+      constexpr int kAhead = kRowLds ? 1 : 4;   // vectors read ahead
+      u32x4 next[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) next[j] = vec(min(tid + j * kThreads, nvec - 1));
       for (int v = tid; v < nvec; v += kThreads) {
-        const u32x4 x = vec(v);
+        const u32x4 x = next[0];
+#pragma unroll
+        for (int j = 0; j + 1 < kAhead; ++j) next[j] = next[j + 1];
+        next[kAhead - 1] = vec(min(v + kAhead * kThreads, nvec - 1));
         u64 w[kPer];
         double exact[kPer];
 #pragma unroll
