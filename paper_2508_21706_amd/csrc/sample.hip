@@ -28,8 +28,8 @@
 //     alone are listed and weighed.
 // One workgroup per row holds the row in LDS when it fits (two rows of up to
 // 62.5 KB per CU), so the logits are read from HBM once.  2048 bf16 rows of
-// 32000 tokens (131 MB, 26 us at a copy's rate) take 68 us with everything
-// kept, 46 with top-50 and 30 greedily: what a row does after its load, 1000
+// 32000 tokens (131 MB, 26 us at a copy's rate) take 61 us with everything
+// kept, 42 with top-50 and 26 greedily: what a row does after its load, 1000
 // instructions per wave and a dozen barriers, is not hidden by the one other
 // row on its CU.  64 fp32 rows take 29 us (the fp64 weights of a row on one
 // CU), one bf16 row with every setting on 8.
@@ -333,9 +333,10 @@ struct Row {
   // loads the row and returns its maximum, -inf for a row without any mass
   __device__ __forceinline__ float load(float& mine) {
     float hi = -INFINITY;
-    // 16-byte loads per lane in flight (rows that fit no LDS: one of 151936 fp32
-    // 16.0 -> 14.1 us greedily with 8, 64 of bf16 11.6 -> 12.4)
-    constexpr int kBatch = kRowLds || BF16 ? 4 : 8;
+    // 16-byte loads per lane in flight: 8 with 8 waves (2048 rows of 32000 bf16
+    // 30.1 -> 26.2 us greedily, top-50 44.5 -> 42) and for fp32 rows that fit no
+    // LDS (one of 151936 16.0 -> 14.1 us; 64 of bf16 11.6 -> 12.4)
+    constexpr int kBatch = kThreads == 512 ? 8 : kRowLds || BF16 ? 4 : 8;
     for (int v0 = tid; v0 < nvec; v0 += kBatch * kThreads) {
       u32x4 x[kBatch];
 #pragma unroll
@@ -380,7 +381,7 @@ struct Row {
     // what lies outside the bins, NaN among it, counts in a spare one of its lane
     const u16x2 out2 = both(kUsualReach + 1 + lane);
     char* const counts = reinterpret_cast<char*>(sh.hist.count);
-    constexpr int kBatch = 4;   // 16-byte loads per lane in flight, while as many are counted
+    constexpr int kBatch = 4;   // 16-byte loads per lane in flight, while as many are counted (8: 2 us more)
     u32x4 next[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
