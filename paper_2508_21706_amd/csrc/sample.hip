@@ -373,7 +373,7 @@ struct Row {
   // largest pattern, and in `near` which of the thread's vectors hold tokens
   // around 0.  (load() and fill() one after the other took 12 instructions per
   // token, not 8, and nothing overlapped the loads: 2048 rows of 32000, 80 us
-  // with everything kept and 79 with top-p 0.9, now 68 and 68.)
+  // with everything kept and 79 with top-p 0.9, then 68 and 68.)
   __device__ __forceinline__ int load_counting(uint32_t& near) {
     typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
     typedef __attribute__((ext_vector_type(2))) short i16x2;
