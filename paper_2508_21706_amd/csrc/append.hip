@@ -14,7 +14,7 @@
 //     one turn in fp64, then one fp32 sine and cosine each.
 // 10,900 tokens of 8 prompts (32 + 2 x 8 heads of 128, bf16) move their 268 MB
 // in 51 us, 5.2 TB/s, what a copy of that size reaches (5.4 TB/s).  A chunk of 5
-// for 64 sequences takes 4.5 us on the GPU and one sequence's 2.8 us, of which
+// for 64 sequences takes 5.2 us on the GPU and one sequence's 2.5 us, of which
 // most are the chain of lengths, table, angle and stores; the calls' host side
 // (9 to 11 us) is longer.
 #include <hip/hip_runtime.h>

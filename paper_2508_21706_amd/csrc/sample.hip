@@ -31,7 +31,7 @@
 // 32000 tokens (131 MB, 26 us at a copy's rate) take 61 us with everything
 // kept, 42 with top-50 and 26 greedily: what a row does after its load, 1000
 // instructions per wave and a dozen barriers, is not hidden by the one other
-// row on its CU.  64 fp32 rows take 29 us (the fp64 weights of a row on one
+// row on its CU.  64 fp32 rows take 28 us (the fp64 weights of a row on one
 // CU), one bf16 row with every setting on 8.
 #include <hip/hip_runtime.h>
 
