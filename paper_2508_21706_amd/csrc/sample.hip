@@ -685,7 +685,7 @@ struct Row {
     static_assert(sizeof(sh.hist) >= kParts * 12, "room for the ranges");
     int* const count = reinterpret_cast<int*>(&sh.hist);
     u64* const mass = reinterpret_cast<u64*>(count + kParts);
-    while (n > kList && lo != hi) {   // (ten bits of the key each time)
+    for (int level = 0; level < 4 && n > kList && lo != hi; ++level) {   // (ten bits of the key each)
       const uint32_t span = hi - lo;
       const int shift = max(0, 32 - __builtin_clz(span) - 10);   // span >> shift < kParts
       __syncthreads();
