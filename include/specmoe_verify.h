@@ -138,8 +138,8 @@ typedef struct specmoe_verify_desc {
  *   lse        float32 [B, C_max, Hq]: natural-log log-sum-exp of the scaled,
  *              masked scores of each row.
  *              (Infinities and NaN in a sequence's valid inputs can reach
- *              all its rows of the same KV head, also rows that do not see
- *              them, and no others.)
+ *              all its rows of the same KV head that see any key, also rows
+ *              that do not see them, and no others.)
  *   stream     hipStream_t the work is enqueued on (NULL: the null stream).
  *   desc       host pointer to the problem description.
  * Padding rows (c_b <= i < C_max) get out = 0 and lse = -inf.  A sequence with

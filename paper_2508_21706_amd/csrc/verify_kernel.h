@@ -1557,9 +1557,10 @@ __global__ __launch_bounds__(kThreads, 1) void verify_attn_kernel(ParamsOf<SCORE
       pend = true;
       pend_whole = whole;
       pend_ok = active && row_valid;
-      // a piece of which a row sees no key leaves that row 0 (at lse -inf),
-      // whatever V holds there: the merge weighs it 0, and 0 x Inf is NaN
-      if (!whole && __any(pend_ok && fl == 0.f)) {
+      // a row that sees no key is left 0 (at lse -inf) whatever V holds there,
+      // in a piece, which the merge weighs 0 (0 x Inf is NaN), as in a whole
+      // unit; a chain's tokens see a whole unit's first key at the least
+      if ((TREE || !whole) && __any(pend_ok && fl == 0.f)) {
 #pragma unroll
         for (int u = 0; u < C::kDB; ++u)
           if (fl == 0.f) o[u] = f32x4{0.f, 0.f, 0.f, 0.f};
