@@ -207,6 +207,7 @@ struct Row {
   static constexpr int kPer = 16 / kElt;             // logits per 16-byte vector
   static constexpr int kBins = BF16 ? 4096 : 2048;   // fp32 ones have a mass of 8 bytes each beside the count
   static constexpr int kOwn = kBins / kThreads;      // bins per thread
+  static constexpr int kGroup = BF16 ? 8 : kOwn;     // patterns of one sign and octave, whatever kThreads
   static constexpr int kDrop = BF16 ? 16 : 17;       // key bits that a bin does not look at
   static constexpr int kZero = 0x80000000u >> kDrop; // the bin pattern of +0; -0 has the one below
 
@@ -239,9 +240,10 @@ struct Row {
   double cut;        // min_p in weight units (0: off)
   // The bins of the patterns K (keys without their last bits), in order: those
   // from base (top, the maximum's, rounded up to a whole group) down to base -
-  // reach.  A thread's bins, a group, are patterns of one sign and octave.
-  // Where there are too many, those around 0 share the group `mid` (-1: none),
-  // `first` the first and `skip` the one kOwn before the last of their places.
+  // reach.  A thread's bins are patterns of one group.  Where there are too
+  // many, whole groups around 0 share the kOwn bins from `mid` on (-1: none),
+  // down to the pattern base - skip - kOwn + 1.  Layouts, and so what shares
+  // bins, do not depend on kThreads for bf16.
   int top, base, reach, mid, skip;
 
   __device__ __forceinline__ Row(const Params& p_, Shared& sh_, const char* src_)
@@ -322,6 +324,7 @@ struct Row {
     return __hiloint2double(__double2hiint(q) + ((units - __double2loint(t)) << 20), __double2loint(q));
   }
   static __device__ __forceinline__ u64 whole(double exact) {
+#pragma clang fp contract(off)   // (no rounding less where `exact` is a product)
     return (u64)__double_as_longlong(exact + 4503599627370496.0) & 0xfffffffffffffull;
   }
   // weight in units, and the same before it was rounded (finite maximum)
@@ -362,10 +365,10 @@ struct Row {
 
   // (bf16) The bins of most rows, laid before the maximum is known: all
   // patterns of kAround <= |x| < 64, those nearer to 0 in one group.
-  static constexpr int kUsualBase = 0xc27f, kUsualMid = kBins / 2 - kOwn;   // (just below 64)
+  static constexpr int kUsualBase = 0xc27f, kUsualMid = kBins / 2 - kGroup;   // (just below 64)
   static constexpr int kAround = kUsualBase + 1 - kZero - kUsualMid;        // (a pattern: 2^-10)
   static constexpr int kUsualSkip = kUsualBase + 1 - kZero + kAround - kOwn;
-  static constexpr int kUsualReach = kUsualSkip + kOwn + kBins / 2 - 1;
+  static constexpr int kUsualReach = kUsualSkip + kBins - 1 - kUsualMid;
   static constexpr int kNearShift = kRowLds ? 0 : 2;   // vectors of a thread per bit, as a power of two: up to 128 of them
   static_assert(!BF16 || ((kMaxVocab / 8 / kThreads) >> kNearShift) <= 32 || kRowLds > 0, "a bit for each");
 
@@ -491,7 +494,7 @@ struct Row {
     top = uniform((int)(key_of(m) >> kDrop));
     int bottom = min(uniform((int)(key_of(least) >> kDrop)), top);
     if (bottom == kZero) --bottom;   // -0 with 0
-    base = top | (kOwn - 1);
+    base = top | (kGroup - 1);
     reach = base - bottom;
     mid = -1;
     skip = reach + 1;
@@ -499,9 +502,9 @@ struct Row {
       // patterns at least a (a whole group) away from 0's on either side keep
       // their bins
       const int above = base + 1 - kZero, below = kZero - bottom;
-      int a = (above + below + kOwn - kBins + 1) / 2;
-      if (a > min(above, below)) a = max(above, below) + kOwn - kBins;
-      a = (a + kOwn - 1) / kOwn * kOwn;
+      int a = (above + below + kGroup - kBins + 1) / 2;
+      if (a > min(above, below)) a = max(above, below) + kGroup - kBins;
+      a = (a + kGroup - 1) / kGroup * kGroup;
       mid = max(base + 1 - (kZero + a), 0);
       skip = base - (kZero - 1 - a) - kOwn;
     }
@@ -782,8 +785,9 @@ struct Row {
     return at < (double)mass ? min((u64)at, mass - 1) : mass - 1;
   }
 
-  // log of a token's share of the kept mass
+  // log of a token's share of the kept mass (the same operations in every kernel)
   __device__ __forceinline__ float log_share(float x, u64 kept) const {
+#pragma clang fp contract(off)
     const double d = ((double)x - md) * (c * 0.69314718055994530942);
     return (float)(d - log((double)kept * (1.0 / (double)(1ull << kUnit))));
   }
@@ -977,7 +981,8 @@ struct Row {
     // most rows whose tokens all have to be weighed are counted as they are
     // loaded, into the usual bins (those with a maximum of 64 or more, or NaN of
     // that sign, or weight below the bins, once more below)
-    const bool all = BF16 && T > 0.f && k != 1 && !(by_k && k <= kBest) && !(by_p && !(top_p > 0.f));
+    const bool best = by_k && k <= kBest;
+    const bool all = BF16 && T > 0.f && k != 1 && !best && !(by_p && !(top_p > 0.f));
     bool usual = false;
     if (all) {
       top = load_counting(near);
@@ -1025,7 +1030,6 @@ struct Row {
       weigh_near(near);
     } else {
       lay_bins(T);
-      const bool best = by_k && k <= kBest;
       if (best && draw_best(u, k, by_p, top_p, mine, token, logp)) return;
       if (all || best) {
         __syncthreads();
@@ -1058,20 +1062,32 @@ struct Row {
     }
     if constexpr (BF16) {
       // A group's values lie at one distance: the first weight (the maximum's,
-      // where it is among them) and a ratio give all (a weight of its own for
-      // each bin took 2900 of a row's 17,000 instructions per CU).
+      // where it is among them) and a ratio give all, by the same products
+      // whatever a thread's part of the group is (a weight of its own for each
+      // bin: 2048 rows 59 -> 63 us).
       const int K0 = pattern_of(tid * kOwn), from = is_mid ? 0 : K0 - min(K0, top);
-      double w0, ratio;
-      weight(value_at(min(K0, top)), w0);
-      ratio = power(((double)value_at(K0 - (kOwn - 2)) - (double)value_at(K0 - (kOwn - 1))) * c, 0);
+      const int first = min(K0 | (kGroup - 1), top), last = K0 & ~(kGroup - 1), steps = first - min(K0, top);
+      double w, ratio, exact[kOwn];
+      weight(value_at(first), w);
+      ratio = power(((double)value_at(last + 1) - (double)value_at(last)) * c, 0);
+#pragma unroll
+      for (int n = 0; n < kGroup - kOwn; ++n) w = n < steps ? w * ratio : w;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) {
+        exact[i] = w;
+        w = i >= from ? w * ratio : w;
+      }
+      if (best) {   // (rarely: draw_best's weights, as the number of threads decides which rows end there)
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) weight(value_at(K0 - i), exact[i]);
+      }
 #pragma unroll
       for (int i = 0; i < kOwn; ++i) {
         const bool there = i >= from;   // (above the maximum there are only NaN)
-        mass[i] = there ? whole(w0) * (u64)count[i] : 0;
+        mass[i] = there ? whole(exact[i]) * (u64)count[i] : 0;
         count[i] = there ? count[i] : 0;
-        if (count[i] && w0 >= cut) own_above = w_own + mass[i];
+        if (count[i] && exact[i] >= cut) own_above = w_own + mass[i];
         w_own += mass[i];
-        w0 = there ? w0 * ratio : w0;
       }
       if (is_mid) {
         w_own = sh.middle;
