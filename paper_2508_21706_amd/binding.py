@@ -194,6 +194,25 @@ def key_tile(desc: Desc) -> int:
     return int(load_library().specmoe_verify_attn_key_tile(ctypes.byref(desc)))
 
 
+_current_gpu = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _status_on(gpu: int, call, *args) -> int:
+    """The status of a library call made with GPU ``gpu`` (a tensor's get_device())
+    current: handle 0 is the null stream of the current GPU, whichever that is."""
+    if gpu == _current_gpu():
+        return call(*args)
+    with torch.cuda.device(gpu):
+        return call(*args)
+
+
+def _launch(gpu: int, call, *args):
+    """A library call with GPU ``gpu`` current; raises on an error status."""
+    st = _status_on(gpu, call, *args)
+    if st != 0:
+        raise SpecMoEError(st, status_str(st))
+
+
 def alloc_workspace(desc: Desc, device, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Allocate a workspace for ``desc`` and zero its status word and counters
     on the stream.  The memory comes from the stream's own pool of the caching
@@ -205,9 +224,8 @@ def alloc_workspace(desc: Desc, device, stream: Optional[torch.cuda.Stream] = No
     s = stream if stream is not None else torch.cuda.current_stream(device)
     with torch.cuda.stream(s):
         ws = torch.empty(n, dtype=torch.uint8, device=device)
-    st = load_library().specmoe_verify_attn_workspace_init(ws.data_ptr(), n, s.cuda_stream, ctypes.byref(desc))
-    if st != 0:
-        raise SpecMoEError(st, status_str(st))
+    _launch(ws.get_device(), load_library().specmoe_verify_attn_workspace_init, ws.data_ptr(), n, s.cuda_stream,
+            ctypes.byref(desc))
     return ws
 
 
@@ -221,8 +239,8 @@ def workspace_status(workspace: Optional[torch.Tensor], stream: Optional[torch.c
         st = load_library().specmoe_verify_attn_status(None, 0, s.cuda_stream)
     else:
         s = stream if stream is not None else torch.cuda.current_stream(workspace.device)
-        st = load_library().specmoe_verify_attn_status(workspace.data_ptr(),
-                                                        workspace.numel() * workspace.element_size(), s.cuda_stream)
+        st = _status_on(workspace.get_device(), load_library().specmoe_verify_attn_status, workspace.data_ptr(),
+                        workspace.numel() * workspace.element_size(), s.cuda_stream)
     if st not in (0, -15):
         raise SpecMoEError(st, status_str(st))
     return st
@@ -307,11 +325,9 @@ def verify_attn_noalloc(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.T
     _check(out, "out", (B, C_max, Hq, D), torch.float32)
     _check(lse, "lse", (B, C_max, Hq), torch.float32)
     desc = make_desc(B, Hq, Hkv, D, C_max, S_max, _dtype_code(q), grid_blocks)
-    st = lib.specmoe_verify_attn_noalloc(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), ctx_lens.data_ptr(),
-                                         chunk_lens.data_ptr(), float(scale), out.data_ptr(), lse.data_ptr(),
-                                         _raw_stream(q, stream), ctypes.byref(desc))
-    if st != 0:
-        raise SpecMoEError(st, status_str(st))
+    _launch(q.get_device(), lib.specmoe_verify_attn_noalloc, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+            ctx_lens.data_ptr(), chunk_lens.data_ptr(), float(scale), out.data_ptr(), lse.data_ptr(),
+            _raw_stream(q, stream), ctypes.byref(desc))
     return out, lse
 
 
@@ -399,24 +415,20 @@ def _call(q, k_cache, v_cache, ctx_lens, chunk_lens, draft_mask, scale, out, lse
         workspace = alloc_workspace(desc, q.device, stream)
     desc.workspace = workspace.data_ptr()
     desc.workspace_bytes = workspace.nbytes
-    raw = _raw_stream(q, stream)
+    gpu, raw = q.get_device(), _raw_stream(q, stream)
     if paged is not None:
-        st = lib.specmoe_verify_attn_paged(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                                           block_table.data_ptr(), ctx_lens.data_ptr(), chunk_lens.data_ptr(),
-                                           draft_mask.data_ptr() if draft_mask is not None else None,
-                                           float(scale), out.data_ptr(), lse.data_ptr(), raw,
-                                           ctypes.byref(desc), ctypes.byref(paged))
+        _launch(gpu, lib.specmoe_verify_attn_paged, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                block_table.data_ptr(), ctx_lens.data_ptr(), chunk_lens.data_ptr(),
+                draft_mask.data_ptr() if draft_mask is not None else None, float(scale), out.data_ptr(),
+                lse.data_ptr(), raw, ctypes.byref(desc), ctypes.byref(paged))
     elif draft_mask is None:
-        st = lib.specmoe_verify_attn(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                                     ctx_lens.data_ptr(), chunk_lens.data_ptr(), float(scale),
-                                     out.data_ptr(), lse.data_ptr(), raw, ctypes.byref(desc))
+        _launch(gpu, lib.specmoe_verify_attn, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                ctx_lens.data_ptr(), chunk_lens.data_ptr(), float(scale), out.data_ptr(), lse.data_ptr(), raw,
+                ctypes.byref(desc))
     else:
-        st = lib.specmoe_verify_attn_tree(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                                          ctx_lens.data_ptr(), chunk_lens.data_ptr(), draft_mask.data_ptr(),
-                                          float(scale), out.data_ptr(), lse.data_ptr(), raw,
-                                          ctypes.byref(desc))
-    if st != 0:
-        raise SpecMoEError(st, status_str(st))
+        _launch(gpu, lib.specmoe_verify_attn_tree, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                ctx_lens.data_ptr(), chunk_lens.data_ptr(), draft_mask.data_ptr(), float(scale), out.data_ptr(),
+                lse.data_ptr(), raw, ctypes.byref(desc))
     return out, lse
 
 
@@ -435,9 +447,7 @@ def alloc_accept_workspace(desc: AcceptDesc, device, stream: Optional[torch.cuda
     s = stream if stream is not None else torch.cuda.current_stream(device)
     with torch.cuda.stream(s):   # from the stream's pool (see alloc_workspace)
         ws = torch.empty(n, dtype=torch.uint8, device=device)
-    st = lib.specmoe_accept_workspace_init(ws.data_ptr(), n, s.cuda_stream, ctypes.byref(desc))
-    if st != 0:
-        raise SpecMoEError(st, status_str(st))
+    _launch(ws.get_device(), lib.specmoe_accept_workspace_init, ws.data_ptr(), n, s.cuda_stream, ctypes.byref(desc))
     return ws
 
 
@@ -474,10 +484,8 @@ def compact_accepted_kv(k_cache: torch.Tensor, v_cache: torch.Tensor, ctx_lens: 
     _check(ctx_lens, "ctx_lens", (B,), torch.int32)
     _check(path, "path", (B,), path.dtype if path.dtype in (torch.int64, torch.uint64) else torch.int64)
     desc = make_desc(B, Hkv, Hkv, D, 1, S_max, _dtype_code(k_cache))
-    st = lib.specmoe_compact_accepted_kv(k_cache.data_ptr(), v_cache.data_ptr(), ctx_lens.data_ptr(), path.data_ptr(),
-                                         _raw_stream(k_cache, stream), ctypes.byref(desc))
-    if st != 0:
-        raise SpecMoEError(st, status_str(st))
+    _launch(k_cache.get_device(), lib.specmoe_compact_accepted_kv, k_cache.data_ptr(), v_cache.data_ptr(),
+            ctx_lens.data_ptr(), path.data_ptr(), _raw_stream(k_cache, stream), ctypes.byref(desc))
 
 
 def accept_greedy(logits: torch.Tensor, tokens: torch.Tensor, ctx_lens: torch.Tensor, chunk_lens: torch.Tensor,
@@ -518,20 +526,16 @@ def accept_greedy(logits: torch.Tensor, tokens: torch.Tensor, ctx_lens: torch.Te
         workspace = alloc_accept_workspace(desc, dev, stream)
     desc.workspace = workspace.data_ptr()
     desc.workspace_bytes = workspace.nbytes
-    raw = _raw_stream(logits, stream)
+    gpu, raw = logits.get_device(), _raw_stream(logits, stream)
     if _tree is None:
-        st = lib.specmoe_accept_greedy(logits.data_ptr(), tokens.data_ptr(), ctx_lens.data_ptr(),
-                                       chunk_lens.data_ptr(), out["argmax"].data_ptr(), out["accepted"].data_ptr(),
-                                       out["next_token"].data_ptr(), out["new_ctx_lens"].data_ptr(), raw,
-                                       ctypes.byref(desc))
+        _launch(gpu, lib.specmoe_accept_greedy, logits.data_ptr(), tokens.data_ptr(), ctx_lens.data_ptr(),
+                chunk_lens.data_ptr(), out["argmax"].data_ptr(), out["accepted"].data_ptr(),
+                out["next_token"].data_ptr(), out["new_ctx_lens"].data_ptr(), raw, ctypes.byref(desc))
     else:
-        st = lib.specmoe_accept_greedy_tree(logits.data_ptr(), tokens.data_ptr(), _tree[0].data_ptr(),
-                                            ctx_lens.data_ptr(), chunk_lens.data_ptr(), out["argmax"].data_ptr(),
-                                            out["accepted"].data_ptr(), out["next_token"].data_ptr(),
-                                            out["new_ctx_lens"].data_ptr(), _tree[1].data_ptr(), raw,
-                                            ctypes.byref(desc))
-    if st != 0:
-        raise SpecMoEError(st, status_str(st))
+        _launch(gpu, lib.specmoe_accept_greedy_tree, logits.data_ptr(), tokens.data_ptr(), _tree[0].data_ptr(),
+                ctx_lens.data_ptr(), chunk_lens.data_ptr(), out["argmax"].data_ptr(), out["accepted"].data_ptr(),
+                out["next_token"].data_ptr(), out["new_ctx_lens"].data_ptr(), _tree[1].data_ptr(), raw,
+                ctypes.byref(desc))
     return out
 
 
@@ -544,20 +548,6 @@ def _check_on(t: torch.Tensor, name: str, shape, dtype, gpu: int):
         return
     _check(t, name, shape, dtype)
     raise ValueError(f"{name} is on {t.device}, expected cuda:{gpu}")
-
-
-_current_gpu = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-
-
-def _launch(gpu: int, call, *args):
-    """A library call with GPU ``gpu`` current; raises on an error status."""
-    if gpu == _current_gpu():
-        st = call(*args)
-    else:
-        with torch.cuda.device(gpu):
-            st = call(*args)
-    if st != 0:
-        raise SpecMoEError(st, status_str(st))
 
 
 def _ptr(t: Optional[torch.Tensor]):
