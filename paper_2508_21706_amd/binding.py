@@ -213,6 +213,17 @@ def _launch(gpu: int, call, *args):
         raise SpecMoEError(st, status_str(st))
 
 
+def _use_workspace(desc, workspace: torch.Tensor, gpu: int):
+    """Put ``workspace`` into ``desc``; the kernels write it, so it has to be
+    memory of GPU ``gpu``."""
+    if workspace.get_device() != gpu or gpu < 0:
+        raise ValueError(f"workspace is on {workspace.device}, expected cuda:{gpu}")
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    desc.workspace = workspace.data_ptr()
+    desc.workspace_bytes = workspace.nbytes
+
+
 def alloc_workspace(desc: Desc, device, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Allocate a workspace for ``desc`` and zero its status word and counters
     on the stream.  The memory comes from the stream's own pool of the caching
@@ -238,6 +249,8 @@ def workspace_status(workspace: Optional[torch.Tensor], stream: Optional[torch.c
         s = stream if stream is not None else torch.cuda.current_stream()
         st = load_library().specmoe_verify_attn_status(None, 0, s.cuda_stream)
     else:
+        if not workspace.is_cuda:
+            raise ValueError(f"workspace is on {workspace.device}, expected a GPU")
         s = stream if stream is not None else torch.cuda.current_stream(workspace.device)
         st = _status_on(workspace.get_device(), load_library().specmoe_verify_attn_status, workspace.data_ptr(),
                         workspace.numel() * workspace.element_size(), s.cuda_stream)
@@ -413,9 +426,8 @@ def _call(q, k_cache, v_cache, ctx_lens, chunk_lens, draft_mask, scale, out, lse
         return out, lse
     if workspace is None:
         workspace = alloc_workspace(desc, q.device, stream)
-    desc.workspace = workspace.data_ptr()
-    desc.workspace_bytes = workspace.nbytes
     gpu, raw = q.get_device(), _raw_stream(q, stream)
+    _use_workspace(desc, workspace, gpu)
     if paged is not None:
         _launch(gpu, lib.specmoe_verify_attn_paged, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
                 block_table.data_ptr(), ctx_lens.data_ptr(), chunk_lens.data_ptr(),
@@ -524,9 +536,8 @@ def accept_greedy(logits: torch.Tensor, tokens: torch.Tensor, ctx_lens: torch.Te
         return out
     if workspace is None:
         workspace = alloc_accept_workspace(desc, dev, stream)
-    desc.workspace = workspace.data_ptr()
-    desc.workspace_bytes = workspace.nbytes
     gpu, raw = logits.get_device(), _raw_stream(logits, stream)
+    _use_workspace(desc, workspace, gpu)
     if _tree is None:
         _launch(gpu, lib.specmoe_accept_greedy, logits.data_ptr(), tokens.data_ptr(), ctx_lens.data_ptr(),
                 chunk_lens.data_ptr(), out["argmax"].data_ptr(), out["accepted"].data_ptr(),
@@ -715,8 +726,7 @@ def verify_attn_scored(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Te
     if B > 0:
         if workspace is None:
             workspace = alloc_workspace(desc, q.device, stream)
-        desc.workspace = workspace.data_ptr()
-        desc.workspace_bytes = workspace.nbytes
+        _use_workspace(desc, workspace, dev)
     window = max(min(window, (1 << 31) - 1), -1)   # (the field has 32 bits, and so has a length)
     score = Score(softcap, window, _ptr(slopes), _ptr(starts))
     _launch(dev, lib.specmoe_verify_attn_scored, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
@@ -811,8 +821,7 @@ def accept_sample(logits: torch.Tensor, tokens: torch.Tensor, ctx_lens: torch.Te
         return out
     if workspace is None:
         workspace = alloc_accept_workspace(desc, logits.device, stream)
-    desc.workspace = workspace.data_ptr()
-    desc.workspace_bytes = workspace.nbytes
+    _use_workspace(desc, workspace, dev)
     head = (logits.data_ptr(), tokens.data_ptr())
     lens = (ctx_lens.data_ptr(), chunk_lens.data_ptr(), uniforms.data_ptr(), ctypes.byref(settings),
             out["sampled"].data_ptr(), out["logprobs"].data_ptr(), out["accepted"].data_ptr(),
