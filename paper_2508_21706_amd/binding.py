@@ -729,6 +729,8 @@ def verify_attn_scored(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Te
         _use_workspace(desc, workspace, dev)
     window = max(min(window, (1 << 31) - 1), -1)   # (the field has 32 bits, and so has a length)
     score = Score(softcap, window, _ptr(slopes), _ptr(starts))
+    if softcap and not score.softcap:   # (0 in 32 bits, which would mean off)
+        raise SpecMoEError(-17, status_str(-17))
     _launch(dev, lib.specmoe_verify_attn_scored, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
             _ptr(block_table), ctx_lens.data_ptr(), chunk_lens.data_ptr(), _ptr(draft_mask), float(scale),
             out.data_ptr(), lse.data_ptr(), _raw_stream(q, stream), ctypes.byref(desc),
