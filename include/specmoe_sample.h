@@ -26,8 +26,9 @@
  *
  * Weights are computed in fp64 and summed as 64-bit integers, in units of
  * 2^-42 of the best token's: sums are exact, so a result depends neither on
- * the order of the additions nor on timing.  A token below half a unit is
- * never drawn and adds nothing to a mass, borders of top_p included.
+ * the order of the additions nor on timing, nor on the other rows of a call.  A
+ * token below half a unit is never drawn and adds nothing to a mass, borders of
+ * top_p included.
  *
  * Status codes are the SPECMOE_* values of specmoe_verify.h.  All functions
  * are plain C; pointers named "device" are HIP device pointers.

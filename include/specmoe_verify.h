@@ -304,6 +304,8 @@ typedef struct specmoe_score {
  *                cache; draft_mask as in specmoe_verify_attn_tree, or NULL.
  *   out          device, 16-byte aligned: [B, C_max, Hq, D] of desc's dtype
  *                (the type that the projection after it takes); not q's memory.
+ *                (As in the other calls, probabilities are rounded to a 16-bit
+ *                dtype for their product with the values.)
  *   score        host pointer to the settings; any of them may be off.
  *
  * A token that sees no key gets out = 0 and lse = -inf, as padding rows do.

@@ -13,7 +13,7 @@
 //     through LDS, while they are under way: the angle and its reduction to
 //     one turn in fp64, then one fp32 sine and cosine each.
 // 10,900 tokens of 8 prompts (32 + 2 x 8 heads of 128, bf16) move their 268 MB
-// in 51 us, 5.2 TB/s, what a copy of that size reaches (5.4 TB/s).  A chunk of 5
+// in 53 us, 5.1 TB/s, near what a copy of that size reaches (5.4 TB/s).  A chunk of 5
 // for 64 sequences takes 5.2 us on the GPU and one sequence's 2.5 us, of which
 // most are the chain of lengths, table, angle and stores; the calls' host side
 // (9 to 11 us) is longer.
@@ -146,8 +146,9 @@ __global__ __launch_bounds__(kMaxThreads) void append_kernel(Params p) {
           const uint64_t seen = p.draft_mask[token] & (c >= kMaxDraftBits ? ~0ull : (1ull << c) - 1);
           pos = l + max((int)__popcll(seen), 1) - 1;
         }
-        // the angle in turns, less its whole turns: exact to 2^-53 of the
-        // angle, so far positions lose nothing in fp32
+        // the angle in turns, less its whole turns: off by at most three
+        // roundings of 2^-53 of the angle (two products, the constant), so far
+        // positions lose nothing in fp32
         double t = (double)pos * p.inv_freq[tid] * 0.15915494309189533577;
         t -= rint(t);
         float sn, cs;

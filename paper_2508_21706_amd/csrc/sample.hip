@@ -28,7 +28,7 @@
 //     alone are listed and weighed.
 // One workgroup per row holds the row in LDS when it fits (two rows of up to
 // 62.5 KB per CU), so the logits are read from HBM once.  2048 bf16 rows of
-// 32000 tokens (131 MB, 26 us at a copy's rate) take 61 us with everything
+// 32000 tokens (131 MB, 26 us at a copy's rate) take 59 us with everything
 // kept, 42 with top-50 and 26 greedily: what a row does after its load, 1000
 // instructions per wave and a dozen barriers, is not hidden by the one other
 // row on its CU.  64 fp32 rows take 28 us (the fp64 weights of a row on one
@@ -56,8 +56,10 @@ constexpr int kUnit = 42;                  // weights are in units of 2^-42
 constexpr double kMost = 43.0;             // from 2^-43 on a weight is less than half a unit
 constexpr int kModeIeee = 1 | (9 << 6);    // s_setreg operand: bit 9 of the MODE register
 
-// Rows of up to kRowSmall bytes (fp32: kRowSmallF32) leave room for two workgroups on a CU, rows up
-// to kRowLarge for one; longer ones are read again from the caches.
+// Rows of up to kRowSmall bytes (fp32: kRowSmallF32, whose bins hold masses too) leave room for two
+// workgroups in a CU's 160 KB of LDS beside 16.3 (24.3) KB of bins and 200 bytes, with 1 (0.5) KB to
+// spare; rows up to kRowLarge for one; longer ones are read again from the caches.
+constexpr int kLds = 160 << 10;
 constexpr int kRowSmall = 64000, kRowSmallF32 = 56320, kRowLarge = 138240;
 
 struct Params {
@@ -186,7 +188,9 @@ __device__ __forceinline__ double scalar(double x) {
 }
 
 // 2^f for |f| <= 1/2: the polynomial of degree 9 through 2^f at the Chebyshev
-// nodes of the interval, off by less than 2^-45.6.
+// nodes of the interval, off by less than 2^-45 absolutely (2^-45.05 at 1/2) and
+// by 2^-44.6 of the value (at -1/2): a quarter of the half unit, 2^-43 of the
+// best token's, by which a weight is rounded.
 __device__ __forceinline__ double exp2_poly(double f) {
   double q = fma(scalar(1.020590550210069e-07), f, scalar(1.3259645241948732e-06));
   q = fma(q, f, scalar(1.5252672924257465e-05));
@@ -1064,7 +1068,7 @@ struct Row {
       // A group's values lie at one distance: the first weight (the maximum's,
       // where it is among them) and a ratio give all, by the same products
       // whatever a thread's part of the group is (a weight of its own for each
-      // bin: 2048 rows 59 -> 63 us).
+      // bin: 2048 rows 57.5 -> 62.6 us).
       const int K0 = pattern_of(tid * kOwn), from = is_mid ? 0 : K0 - min(K0, top);
       const int first = min(K0 | (kGroup - 1), top), last = K0 & ~(kGroup - 1), steps = first - min(K0, top);
       double w, ratio, exact[kOwn];
@@ -1256,6 +1260,7 @@ __device__ __forceinline__ void accept(const Params& p, int b, int c, int lane) 
 template <bool BF16, int kRowLds, int kThreads, bool ACCEPT>
 __global__ __launch_bounds__(kThreads, 4) void sample_kernel(Params p) {
   using R = Row<BF16, kRowLds, kThreads>;
+  static_assert(sizeof(typename R::Shared) <= (kThreads == 512 ? kLds / 2 : kLds), "LDS of a CU");
   __shared__ typename R::Shared sh;
   // MODE.IEEE off: a maximum with one NaN operand, signalling or quiet, is the
   // other operand
