@@ -417,8 +417,7 @@ def _plain_step(st, ctx, chunk):
     source = torch.where(coming, total - 1 - (want_end - want)[:, None] - (j - held[:, None]), 0)
     st["table"].copy_(torch.where(coming, stack[source], table))
     st["held"].copy_(torch.where(served, need, torch.minimum(held, need)))
-    at = torch.arange(n, device=table.device)
-    st["free"].copy_(torch.where((at >= count) & (at < total - taken), stack[:n], free))
+    free.copy_(stack[:n])
     st["count"].copy_(total - taken)
     st["missing"].copy_(torch.where(served, 0, want))
     i = torch.arange(C, device=table.device)
