@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -83,6 +83,24 @@ class Sampling(ctypes.Structure):
                 ("min_p", ctypes.c_void_p)]
 
 
+class KV4(ctypes.Structure):
+    """Mirror of ``specmoe_kv4``."""
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p)]
+
+
+class KV4Desc(ctypes.Structure):
+    """Mirror of ``specmoe_kv4_desc``."""
+    _fields_ = [("B", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32), ("N_max", ctypes.c_int32),
+                ("S_max", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class PagesDesc(ctypes.Structure):
+    """Mirror of ``specmoe_pages_desc``."""
+    _fields_ = [("B", ctypes.c_int32), ("C_max", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("pages_per_seq", ctypes.c_int32), ("num_pages", ctypes.c_int32)]
+
+
 class SpecMoEError(RuntimeError):
     def __init__(self, status: int, text: str):
         super().__init__(f"{STATUS.get(status, status)}: {text}")
@@ -150,6 +168,23 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.specmoe_accept_sample_tree.restype = ctypes.c_int
     lib.specmoe_accept_sample_tree.argtypes = [ctypes.c_void_p] * 6 + [ctypes.POINTER(Sampling)] + [
         ctypes.c_void_p] * 7 + [ctypes.POINTER(AcceptDesc)]
+    lib.specmoe_append_kv4.restype = ctypes.c_int
+    lib.specmoe_append_kv4.argtypes = [ctypes.c_void_p] * 11 + [
+        ctypes.POINTER(KV4), ctypes.c_void_p, ctypes.POINTER(AppendDesc), ctypes.POINTER(PagedKV)]
+    lib.specmoe_verify_attn_kv4.restype = ctypes.c_int
+    lib.specmoe_verify_attn_kv4.argtypes = [ctypes.c_void_p, ctypes.POINTER(KV4)] + [ctypes.c_void_p] * 4 + [
+        ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(Desc),
+        ctypes.POINTER(PagedKV)]
+    lib.specmoe_verify_attn_kv4_workspace_bytes.restype = ctypes.c_size_t
+    lib.specmoe_verify_attn_kv4_workspace_bytes.argtypes = [ctypes.POINTER(Desc)]
+    lib.specmoe_read_kv4.restype = ctypes.c_int
+    lib.specmoe_read_kv4.argtypes = [ctypes.POINTER(KV4)] + [ctypes.c_void_p] * 6 + [
+        ctypes.POINTER(KV4Desc), ctypes.POINTER(PagedKV)]
+    lib.specmoe_compact_accepted_kv4.restype = ctypes.c_int
+    lib.specmoe_compact_accepted_kv4.argtypes = [ctypes.POINTER(KV4)] + [ctypes.c_void_p] * 4 + [
+        ctypes.POINTER(KV4Desc), ctypes.POINTER(PagedKV)]
+    lib.specmoe_assign_pages.restype = ctypes.c_int
+    lib.specmoe_assign_pages.argtypes = [ctypes.c_void_p] * 9 + [ctypes.POINTER(PagesDesc)]
     lib.specmoe_status_str.restype = ctypes.c_char_p
     lib.specmoe_status_str.argtypes = [ctypes.c_int]
     if path is None:
@@ -850,3 +885,284 @@ def accept_sample_tree(logits: torch.Tensor, tokens: torch.Tensor, draft_mask: t
     _check_on(draft_mask, "draft_mask", tuple(tokens.shape), mdt, logits.get_device())
     return accept_sample(logits, tokens, ctx_lens, chunk_lens, uniforms, temperature, top_k, top_p, min_p, out=out,
                          workspace=workspace, stream=stream, in_place=in_place, _tree=draft_mask)
+
+
+# ------------------------------------------------------------- 4-bit cache
+
+class KV4Cache(NamedTuple):
+    """A KV cache held in 4 bits (``include/specmoe_kv4.h``): uint8 codes
+    [.., Hkv, rows, D / 2] and scales [.., Hkv, rows, D / 32] of keys and values,
+    a slab per sequence or a pool of pages."""
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+
+
+def alloc_kv4_cache(slabs: int, Hkv: int, rows: int, D: int, device) -> KV4Cache:
+    """An empty 4-bit cache: ``slabs`` sequences of ``rows`` tokens, or a pool of
+    ``slabs`` pages of ``rows`` tokens.  (All zeros: every entry is 0.)"""
+    new = lambda n: torch.zeros((slabs, Hkv, rows, n), dtype=torch.uint8, device=device)   # noqa: E731
+    return KV4Cache(new(D // 2), new(D // 32), new(D // 2), new(D // 32))
+
+
+def _kv4(cache: KV4Cache, B: int, block_table: Optional[torch.Tensor], gpu: int):
+    """(library struct, Hkv, S_max, D, page geometry or None) of a checked cache."""
+    kc, ks, vc, vs = cache
+    if kc.dim() != 4:
+        raise ValueError("k_codes must be [B, Hkv, S_max, D / 2] or [num_pages, Hkv, page_size, D / 2]")
+    n, Hkv, rows, half = kc.shape
+    codes, scales = (n, Hkv, rows, half), (n, Hkv, rows, half // 16)
+    u8 = torch.uint8
+    _check_on(kc, "k_codes", codes, u8, gpu)
+    _check_on(ks, "k_scales", scales, u8, gpu)
+    _check_on(vc, "v_codes", codes, u8, gpu)
+    _check_on(vs, "v_scales", scales, u8, gpu)
+    ptrs = KV4(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr())
+    if block_table is None:
+        if n != B:
+            raise ValueError(f"the cache has slabs for {n} sequences, expected {B}")
+        return ptrs, Hkv, rows, 2 * half, None
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, pages_per_seq]")
+    per = block_table.shape[1]
+    _check_on(block_table, "block_table", (B, per), torch.int32, gpu)
+    return ptrs, Hkv, rows * per, 2 * half, PagedKV(rows, per, n)
+
+
+def _ref(s):
+    return None if s is None else ctypes.byref(s)
+
+
+def append_kv4(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cache: KV4Cache, ctx_lens: torch.Tensor,
+               chunk_lens: torch.Tensor, inv_freq: Optional[torch.Tensor] = None, rope: str = "halves",
+               q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+               draft_mask: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None,
+               q_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """``append_kv`` into a 4-bit cache; see ``specmoe_append_kv4`` in
+    ``include/specmoe_kv4.h``.  The step before ``verify_attn_kv4``; arguments
+    and result are those of ``append_kv``."""
+    lib = load_library()
+    if k.dim() != 4 or (q is not None and q.dim() != 4):
+        raise ValueError("q, k and v have four dimensions")
+    B, C_max, Hkv, D = k.shape
+    dt, dev = k.dtype, k.get_device()
+    if rope not in ROPE_STYLES:
+        raise ValueError(f"rope must be one of {sorted(ROPE_STYLES)}, got {rope!r}")
+    Hq = 0 if q is None else q.shape[2]
+    ks = _token_stride(k, "k", (B, C_max, Hkv, D), dt, dev)
+    vs = _token_stride(v, "v", (B, C_max, Hkv, D), dt, dev)
+    ptrs, cache_heads, S_max, cache_dim, paged = _kv4(cache, B, block_table, dev)
+    if cache_heads != Hkv or cache_dim != D:
+        raise ValueError(f"the cache has {cache_heads} heads of {cache_dim}, expected {Hkv} of {D}")
+    _check_on(ctx_lens, "ctx_lens", (B,), torch.int32, dev)
+    _check_on(chunk_lens, "chunk_lens", (B,), torch.int32, dev)
+    qs = 0
+    if q is not None:
+        qs = _token_stride(q, "q", (B, C_max, Hq, D), dt, dev)
+        if q_out is None:
+            q_out = _empty((B, C_max, Hq, D), dt, k.device, stream)
+        else:
+            _check_on(q_out, "q_out", (B, C_max, Hq, D), dt, dev)
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _check_on(w, name, (D,), dt, dev)
+    rot_dim = 0
+    if inv_freq is not None:
+        _check_on(inv_freq, "inv_freq", (inv_freq.numel(),), torch.float64, dev)
+        rot_dim = 2 * inv_freq.numel()
+    if draft_mask is not None:
+        mdt = draft_mask.dtype if draft_mask.dtype in (torch.int64, torch.uint64) else torch.int64
+        _check_on(draft_mask, "draft_mask", (B, C_max), mdt, dev)
+    desc = AppendDesc(B, Hq, Hkv, D, C_max, S_max, _dtype_code(k), rot_dim, ROPE_STYLES[rope], eps, qs, ks, vs)
+    _launch(dev, lib.specmoe_append_kv4, _ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_weight), _ptr(k_weight),
+            _ptr(inv_freq), ctx_lens.data_ptr(), chunk_lens.data_ptr(), _ptr(draft_mask), _ptr(block_table),
+            _ptr(q_out) if q is not None else None, ctypes.byref(ptrs), _raw_stream(k, stream), ctypes.byref(desc),
+            _ref(paged))
+    return q_out if q is not None else None
+
+
+def alloc_kv4_workspace(q: torch.Tensor, cache: KV4Cache, block_table: Optional[torch.Tensor] = None,
+                        grid_blocks: int = 0, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """A workspace for ``verify_attn_kv4`` calls of these shapes; as it is at least
+    as large as ``alloc_workspace``'s, it serves ``verify_attn`` too."""
+    if q.dim() != 4 or cache.k_codes.dim() != 4:
+        raise ValueError("q and the cache's tensors have four dimensions")
+    B, C_max, Hq, D = q.shape
+    _, Hkv, rows, _ = cache.k_codes.shape
+    S_max = rows if block_table is None else rows * block_table.shape[1]
+    desc = make_desc(B, Hq, Hkv, D, C_max, S_max, _dtype_code(q), grid_blocks)
+    return _alloc_kv4_workspace(desc, q.device, stream)
+
+
+def _alloc_kv4_workspace(desc: Desc, device, stream) -> torch.Tensor:
+    lib = load_library()
+    n = int(lib.specmoe_verify_attn_kv4_workspace_bytes(ctypes.byref(desc)))
+    if n == 0:
+        raise SpecMoEError(-2, "invalid descriptor")
+    s = stream if stream is not None else torch.cuda.current_stream(device)
+    with torch.cuda.stream(s):   # from the stream's pool (see alloc_workspace)
+        ws = torch.empty(n, dtype=torch.uint8, device=device)
+    _launch(ws.get_device(), lib.specmoe_verify_attn_workspace_init, ws.data_ptr(), n, s.cuda_stream, ctypes.byref(desc))
+    return ws
+
+
+def verify_attn_kv4(q: torch.Tensor, cache: KV4Cache, ctx_lens: torch.Tensor, chunk_lens: torch.Tensor, scale: float,
+                    draft_mask: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None,
+                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, grid_blocks: int = 0,
+                    stream: Optional[torch.cuda.Stream] = None, check_lengths: bool = False):
+    """Verification (C_max = 1: decode) attention over a 4-bit cache; see
+    ``specmoe_verify_attn_kv4`` in ``include/specmoe_kv4.h``.
+
+    q [B, C_max, Hq, D] (bf16, f16 or f32); the other arguments as
+    ``verify_attn``, ``verify_attn_tree`` (``draft_mask``) and
+    ``verify_attn_paged`` (``block_table``).  Returns (out, lse): ``out``
+    [B, C_max, Hq, D] in q's type, ``lse`` float32 [B, C_max, Hq].
+    """
+    lib = load_library()
+    if q.dim() != 4:
+        raise ValueError("q must be [B, C_max, Hq, D]")
+    B, C_max, Hq, D = q.shape
+    dt, dev = q.dtype, q.get_device()
+    _check_on(q, "q", (B, C_max, Hq, D), dt, dev)
+    ptrs, Hkv, S_max, cache_dim, paged = _kv4(cache, B, block_table, dev)
+    if cache_dim != D:
+        raise ValueError(f"the cache has heads of {cache_dim}, expected {D}")
+    _check_on(ctx_lens, "ctx_lens", (B,), torch.int32, dev)
+    _check_on(chunk_lens, "chunk_lens", (B,), torch.int32, dev)
+    if draft_mask is not None:
+        mdt = draft_mask.dtype if draft_mask.dtype in (torch.int64, torch.uint64) else torch.int64
+        _check_on(draft_mask, "draft_mask", (B, C_max), mdt, dev)
+    if check_lengths:
+        c, l = chunk_lens.cpu(), ctx_lens.cpu()
+        if (c < 0).any() or (c > C_max).any() or (l < 0).any() or (l + c > S_max).any():
+            raise ValueError("lengths break 0 <= c_b <= C_max, l_b >= 0, l_b + c_b <= S_max")
+    if out is None:
+        out = _empty((B, C_max, Hq, D), dt, q.device, stream)
+    if lse is None:
+        lse = _empty((B, C_max, Hq), torch.float32, q.device, stream)
+    _check_on(out, "out", (B, C_max, Hq, D), dt, dev)
+    _check_on(lse, "lse", (B, C_max, Hq), torch.float32, dev)
+    desc = make_desc(B, Hq, Hkv, D, C_max, S_max, _dtype_code(q), grid_blocks)
+    if B > 0:
+        if workspace is None:
+            workspace = _alloc_kv4_workspace(desc, q.device, stream)
+        _use_workspace(desc, workspace, dev)
+    _launch(dev, lib.specmoe_verify_attn_kv4, q.data_ptr(), ctypes.byref(ptrs), _ptr(block_table), ctx_lens.data_ptr(),
+            chunk_lens.data_ptr(), _ptr(draft_mask), float(scale), out.data_ptr(), lse.data_ptr(),
+            _raw_stream(q, stream), ctypes.byref(desc), _ref(paged))
+    return out, lse
+
+
+def read_kv4(cache: KV4Cache, first: torch.Tensor, rows: torch.Tensor, max_rows: Optional[int] = None,
+             dtype: torch.dtype = torch.bfloat16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
+             block_table: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Rows of a 4-bit cache as the values they stand for; see
+    ``specmoe_read_kv4`` in ``include/specmoe_kv4.h``.
+
+    ``first`` / ``rows`` int32 [B]: sequence b's rows first_b + i, i < rows_b, go
+    to k_out[b, i] and v_out[b, i], which are [B, max_rows, Hkv, D] of ``dtype``
+    (bf16, f16 or f32); ``out`` may supply the pair, whose other rows stay as
+    they are (new ones hold zeros there).  Returns (k_out, v_out).
+    """
+    lib = load_library()
+    dev = cache.k_codes.get_device()
+    B = first.numel()
+    ptrs, Hkv, S_max, D, paged = _kv4(cache, B, block_table, dev)
+    _check_on(first, "first", (B,), torch.int32, dev)
+    _check_on(rows, "rows", (B,), torch.int32, dev)
+    if out is None:
+        if max_rows is None:
+            raise ValueError("read_kv4 needs max_rows or out")
+        with torch.cuda.stream(stream):   # (None: the current one)
+            out = tuple(torch.zeros((B, max_rows, Hkv, D), dtype=dtype, device=first.device) for _ in range(2))
+    k_out, v_out = out
+    if k_out.dim() != 4:
+        raise ValueError("k_out must be [B, max_rows, Hkv, D]")
+    shape = (B, k_out.shape[1], Hkv, D)
+    _check_on(k_out, "k_out", shape, k_out.dtype, dev)
+    _check_on(v_out, "v_out", shape, k_out.dtype, dev)
+    desc = KV4Desc(B, Hkv, D, shape[1], S_max, _dtype_code(k_out))
+    _launch(dev, lib.specmoe_read_kv4, ctypes.byref(ptrs), _ptr(block_table), first.data_ptr(), rows.data_ptr(),
+            k_out.data_ptr(), v_out.data_ptr(), _raw_stream(first, stream), ctypes.byref(desc), _ref(paged))
+    return k_out, v_out
+
+
+def compact_accepted_kv4(cache: KV4Cache, ctx_lens: torch.Tensor, path: torch.Tensor,
+                         block_table: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Move each sequence's accepted tree path's rows of a 4-bit cache (slabs or,
+    with ``block_table``, pages) to the rows right after its context
+    (``specmoe_compact_accepted_kv4``); ``ctx_lens`` are the lengths from before
+    the acceptance step."""
+    lib = load_library()
+    dev = cache.k_codes.get_device()
+    B = ctx_lens.numel()
+    ptrs, Hkv, S_max, D, paged = _kv4(cache, B, block_table, dev)
+    _check_on(ctx_lens, "ctx_lens", (B,), torch.int32, dev)
+    _check_on(path, "path", (B,), path.dtype if path.dtype in (torch.int64, torch.uint64) else torch.int64, dev)
+    desc = KV4Desc(B, Hkv, D, 0, S_max, 0)
+    _launch(dev, lib.specmoe_compact_accepted_kv4, ctypes.byref(ptrs), _ptr(block_table), ctx_lens.data_ptr(),
+            path.data_ptr(), _raw_stream(ctx_lens, stream), ctypes.byref(desc), _ref(paged))
+
+
+# ------------------------------------------------------------------- pages
+
+class PageState(NamedTuple):
+    """Who holds which page of a pool (``include/specmoe_pages.h``): the block table
+    int32 [B, pages_per_seq], the pages each request holds int32 [B], the stack of
+    free pages int32 [num_pages] and their number int32 [1]."""
+    block_table: torch.Tensor
+    held: torch.Tensor
+    free_pages: torch.Tensor
+    free_count: torch.Tensor
+
+
+def alloc_page_state(B: int, pages_per_seq: int, num_pages: int, device) -> PageState:
+    """All pages free (page 0 the first to be taken), no request holds any."""
+    i32 = dict(dtype=torch.int32, device=device)
+    return PageState(torch.zeros((B, pages_per_seq), **i32), torch.zeros((B,), **i32),
+                     torch.arange(num_pages - 1, -1, -1, **i32), torch.full((1,), num_pages, **i32))
+
+
+def assign_pages(ctx_lens: torch.Tensor, chunk_lens: torch.Tensor, pages: PageState, page_size: int,
+                 missing: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+                 max_chunk: Optional[int] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Give every request the pages that ctx_lens + chunk_lens tokens need and
+    take back those that it no longer does; see ``specmoe_assign_pages`` in
+    ``include/specmoe_pages.h``.  The step before ``append_kv`` and the paged
+    attention calls, whose ``block_table`` is ``pages.block_table``.
+
+    Updates ``pages`` in place.  ``missing`` int32 [B]: pages that a request needs
+    and did not get.  ``slots`` int64 [B, C_max]: the place of each chunk token in
+    the pool (-1: none), for writers that take slot maps; chunks are clamped to
+    C_max (without ``slots``: to ``max_chunk``).  Returns (missing, slots);
+    ``missing`` is allocated if None.
+    """
+    lib = load_library()
+    table, held, free, count = pages
+    if table.dim() != 2 or free.dim() != 1:
+        raise ValueError("block_table must be [B, pages_per_seq], free_pages [num_pages]")
+    B, per = table.shape
+    dev, i32 = table.get_device(), torch.int32
+    _check_on(table, "block_table", (B, per), i32, dev)
+    _check_on(held, "held", (B,), i32, dev)
+    _check_on(free, "free_pages", (free.shape[0],), i32, dev)
+    _check_on(count, "free_count", (1,), i32, dev)
+    _check_on(ctx_lens, "ctx_lens", (B,), i32, dev)
+    _check_on(chunk_lens, "chunk_lens", (B,), i32, dev)
+    if slots is not None:
+        if slots.dim() != 2:
+            raise ValueError("slots must be [B, C_max]")
+        C_max = slots.shape[1]
+        _check_on(slots, "slots", (B, C_max), torch.int64, dev)
+    else:
+        C_max = per * page_size if max_chunk is None else max_chunk
+    if missing is None:
+        missing = _empty((B,), i32, table.device, stream)
+    _check_on(missing, "missing", (B,), i32, dev)
+    desc = PagesDesc(B, C_max, page_size, per, free.shape[0])
+    _launch(dev, lib.specmoe_assign_pages, ctx_lens.data_ptr(), chunk_lens.data_ptr(), table.data_ptr(),
+            held.data_ptr(), free.data_ptr(), count.data_ptr(), missing.data_ptr(), _ptr(slots),
+            _raw_stream(table, stream), ctypes.byref(desc))
+    return missing, slots

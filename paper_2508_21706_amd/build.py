@@ -17,7 +17,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", name) for name in ("verify_attn.hip", "verify_scored.hip", "accept.hip", "append.hip",
-                                                       "sample.hip")]
+                                                       "sample.hip", "kv4.hip", "kv4_attn.hip", "pages.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 OUTPUT = os.path.join(HERE, "libspecmoe_verify.so")
 PROBE_SOURCES = [os.path.join(HERE, "csrc", "stream_probe.hip")]
