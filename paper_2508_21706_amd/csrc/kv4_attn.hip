@@ -16,6 +16,13 @@ constexpr int kGroupThreads = 64 * kGroupWaves;
 constexpr int kGroupsDefault = 512;   // persistent workgroups: two per CU of an MI355X
 constexpr int kTile = 128;            // keys of a tile
 constexpr int kStep = 32;             // keys that a wave takes at a time: two MFMA blocks
+// The schedule (see the kernel): tiles a workgroup from which on units cost and cuts
+// snap, what a unit costs beside its tiles, and how near a unit's end a cut goes to it
+constexpr int kManyTiles = 6, kUnitCost = 2, kSnap = 2;
+
+// Where the cache's rows are: a slab per sequence, or pages of at least 16 tokens (a
+// block of 16 keys is in one page), or of 8
+constexpr int kSlab = 0, kPages = 1, kSmallPages = 2;
 
 struct Kv4Params : Params {   // (k and v: the codes)
   const char* k_scales;
@@ -23,11 +30,42 @@ struct Kv4Params : Params {   // (k and v: the codes)
   int row_groups;   // waves of a workgroup that have different rows: 1, 2 or 4
 };
 
-// bfloat16 parts that a value of the type is the sum of
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+
+// How scores are formed.  kCodes: the key codes go into the MFMA as they are (f8f6f4,
+// scales and all), against queries in 8 bits: a query is cut into parts of 4
+// significant bits, two for bfloat16's 8 and three for float16's 11.  Otherwise
+// (float32, whose 24 bits would take six, and D = 64, half of the MFMA's 128) the
+// codes become bfloat16, against one, two or three bfloat16 parts.
+template <int ELT, int D>
+constexpr bool kCodes = D == 128 && ELT != kF32;
+template <int ELT, int D>
+constexpr int kQParts = kCodes<ELT, D> ? (ELT == kBF16 ? 2 : 3) : ELT == kBF16 ? 1 : ELT == kF16 ? 2 : 3;
+// bfloat16 parts of a probability for its product with the values
 template <int ELT>
-constexpr int kParts = ELT == kBF16 ? 1 : ELT == kF16 ? 2 : 3;
+constexpr int kPParts = ELT == kBF16 ? 1 : ELT == kF16 ? 2 : 3;
+// Binades from one 8-bit part of a query to the next: a part's rounding leaves at most
+// 2^-5 of the largest entry's power of two
+constexpr int kPartShift = 5;
 
 __device__ __forceinline__ int tiles_of(uint32_t s) { return sched::seq_tiles(s, kTile); }
+
+// A workgroup barrier for data in LDS alone: loads and stores under way stay so
+// (__syncthreads() waits for them: 2 us at every unit's end).
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// The largest of 8 scores, NaN aside
+__device__ __forceinline__ float max8(const float (&y)[8]) {
+  float a, b;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(y[0]), "v"(y[1]), "v"(y[2]));
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(b) : "v"(y[3]), "v"(y[4]), "v"(y[5]));
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(a), "v"(y[6]), "v"(y[7]));
+  return fmaxf(a, b);
+}
 
 // Two values cut to their leading 8 significant bits, as two bfloat16; x keeps
 // what was cut off.  Infinities and NaN go whole into the first part.
@@ -41,10 +79,33 @@ __device__ __forceinline__ uint32_t split2(float& x, float& y) {
   return (p >> 16) | q;
 }
 
-template <int ELT, int D, bool PAGED, int NRB>
+// (kCodes) 16 values as 8-bit codes of `unit`, to nearest even; x keeps what the
+// rounding left.  An infinity or NaN has the NaN code.
+__device__ __forceinline__ void part8(float (&x)[16], float unit, bool rest, int* codes) {
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    s16x2 c = {0, 0};
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, x[4 * w], x[4 * w + 1], unit, false);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, x[4 * w + 2], x[4 * w + 3], unit, true);
+    codes[w] = __builtin_bit_cast(int, c);
+    if (rest) {
+      const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes[w], unit, false);
+      const f32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes[w], unit, true);
+      x[4 * w] -= lo[0];
+      x[4 * w + 1] -= lo[1];
+      x[4 * w + 2] -= hi[0];
+      x[4 * w + 3] -= hi[1];
+    }
+  }
+}
+
+template <int ELT, int D, int PAGING, int NRB>
 __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p) {
   constexpr int kElt = ELT == kF32 ? 4 : 2;
-  constexpr int NP = kParts<ELT>;
+  constexpr bool CODES = kCodes<ELT, D>;
+  constexpr int QP = kQParts<ELT, D>, PP = kPParts<ELT>;
   constexpr int KW = D / 32;          // code words of a lane: its D / 4 entries of a row
   constexpr int DB = D / 16;          // 16-wide d blocks of O^T
   constexpr int kPitch = 2 * D + (D == 128 ? 32 : 16);   // LDS bytes of a staged V row, free of bank conflicts
@@ -52,39 +113,52 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
   static_assert(kStage >= kBlk * D * 4, "a row block's O fits a wave's stage");
   __shared__ __attribute__((aligned(16))) char smem[kGroupWaves * kStage];
   __shared__ uint32_t seqs[kMaxSeqs];
-  __shared__ int pref[kMaxSeqs];      // tiles of one KV head of the sequences before b
-  __shared__ int wsum[kGroupWaves];
+  __shared__ int pref[kMaxSeqs];      // cost of one KV head's units of the sequences before b
+  __shared__ int wsum[2][kGroupWaves];
   __shared__ float mst[kGroupWaves][NRB][2][kBlk];
-  __shared__ int sh_flag;
+  __shared__ int sh_last[2];
 
   const int pid = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int lm = lane & 15, lg = lane >> 4;
   const int B = p.B, Hkv = p.Hkv, g = p.g;
   const int RG = p.row_groups, KS = kGroupWaves / RG;   // row groups, waves that share a row group's keys
-  const int rg = wave % RG, kslot = wave / RG;
+  const int rg = wave & (RG - 1), kslot = RG == 1 ? wave : RG == 2 ? wave >> 1 : 0;
 
-  // ---- lengths, tile sums, this workgroup's range [g0, g1) of the list of all
-  // units' tiles
+  // ---- lengths, and this workgroup's range of the list of all units' tiles.
+  // Ranges are of equal cost: a tile costs 1 and a unit's start and end kUnitCost
+  // more.  A range that would begin within kSnap tiles of a unit's start or end
+  // begins there.  With few tiles to a workgroup units cost nothing and are cut
+  // anywhere.
   const int per = (B + kGroupThreads - 1) / kGroupThreads;
   const int b_lo = min(tid * per, B), b_hi = min(b_lo + per, B);
-  int mine = 0;
+  int mine = 0, some = 0;   // tiles, and sequences that have any
   for (int b = b_lo; b < b_hi; ++b) {
     const uint32_t s = load_seq(p, b);
     seqs[b] = s;
     mine += tiles_of(s);
+    some += tiles_of(s) > 0;
   }
-  const int incl = wave_scan(mine);
-  if (lane == 63) wsum[wave] = incl;
+  const int incl = wave_scan(mine), incl_some = wave_scan(some);
+  if (lane == 63) {
+    wsum[0][wave] = incl;
+    wsum[1][wave] = incl_some;
+  }
   __syncthreads();
-  int before = incl - mine, total = 0;
+  int before = incl - mine, before_some = incl_some - some, total = 0, total_some = 0;
 #pragma unroll
   for (int w = 0; w < kGroupWaves; ++w) {
-    before += w < wave ? wsum[w] : 0;
-    total += wsum[w];
+    before += w < wave ? wsum[0][w] : 0;
+    before_some += w < wave ? wsum[1][w] : 0;
+    total += wsum[0][w];
+    total_some += wsum[1][w];
   }
-  for (int b = b_lo; b < b_hi; ++b) {
-    pref[b] = before;
-    before += tiles_of(seqs[b]);
+  const int N = uniform(total) * Hkv;   // tiles (host check)
+  const bool many = N >= kManyTiles * p.P;
+  const int unit_cost = many ? kUnitCost : 0, snap = many ? kSnap : 1;
+  for (int b = b_lo, x = before + unit_cost * before_some; b < b_hi; ++b) {
+    pref[b] = x;
+    const int n = tiles_of(seqs[b]);
+    x += n + (n > 0 ? unit_cost : 0);
   }
   __syncthreads();
 
@@ -102,157 +176,297 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
     }
   }
 
-  const int64_t N = (int64_t)uniform(total) * Hkv;   // (< 2^31: host check)
-  const int P = (int)min((int64_t)p.P, N);
+  // Ranges of cost / P, the first cost % P of them of one more
+  const int cost = N + unit_cost * uniform(total_some) * Hkv;
+  const int P = min(p.P, N);
   if (pid >= P) return;
-  const int g0 = (int)(N * pid / P), g1 = (int)(N * (pid + 1) / P);
-  // the range that has tile t
-  auto owner = [&](int t) { return (int)((((int64_t)t + 1) * P - 1) / N); };
-
-  // the last sequence whose tiles begin at or before g0 (it has some)
-  int b = 0;
-  for (int step = 512; step; step >>= 1)
-    if (b + step < B && (int64_t)pref[b + step] * Hkv <= g0) b += step;
-  b = uniform(b);
+  const int share = uniform(cost / P), longer = cost - share * P;
+  auto range_start = [&](int r) { return r * share + min(r, longer); };
+  // the last range that starts at or before a cost
+  auto owner = [&](int x) {
+    const int cut = longer * (share + 1);
+    return uniform(x < cut ? x / (share + 1) : longer + (x - cut) / share);
+  };
+  // the tile of a unit of n at which a range begins whose cost lies x after the
+  // unit's (0: at its start, n: at the next one's), and the largest such x for its
+  // first tile and for its last one
+  auto cut_at = [&](int x, int n) {
+    const int j = x - unit_cost / 2;
+    if (n < 2 * snap) return 2 * j < n ? 0 : n;
+    return j < snap ? 0 : j > n - snap ? n : j;
+  };
+  auto most_first = [&](int n) { return unit_cost / 2 + (n < 2 * snap ? (n - 1) >> 1 : snap - 1); };
+  auto most_last = [&](int n) { return unit_cost / 2 + (n < 2 * snap ? (n - 1) >> 1 : n - snap); };
+  const int c_end = range_start(pid + 1);
 
   char* const stage = smem + wave * kStage;
 
-  for (int t = g0; t < g1;) {
-    // ---- segment: tiles [j0, j1) of KV head kvh of sequence b
-    uint32_t s = uniform(seqs[b]);
-    int n = tiles_of(s);
-    int rel = t - uniform(pref[b]) * Hkv;
-    while (rel >= n * Hkv) {   // (the next sequence that has tiles)
-      ++b;
-      s = uniform(seqs[b]);
-      n = tiles_of(s);
-      rel = t - uniform(pref[b]) * Hkv;
+  // ---- segments: tiles [j0, j1) of one unit, KV head kvh of sequence b
+  struct Segment {
+    int b, kvh, j0, j1, n, T, c;   // n: tiles of the unit
+    int kend;                      // the first key past the segment
+    int cost;                      // at which the unit begins
+  };
+  // (of the range: j1 = 0 if the unit is past its end)
+  auto segment = [&](int b, int kvh, int j0, int at) {
+    Segment x;
+    const uint32_t s = uniform(seqs[b]);
+    x.b = b;
+    x.kvh = kvh;
+    x.n = tiles_of(s);
+    x.j0 = j0;
+    x.cost = at;
+    x.j1 = c_end >= at + x.n + unit_cost ? x.n : c_end > at ? cut_at(c_end - at, x.n) : 0;
+    x.T = seq_T(s);
+    x.c = seq_c(s);
+    x.kend = min(x.T, x.j1 * kTile);
+    return x;
+  };
+  // the next unit, from its tile 0 (past the last one: no tiles)
+  auto segment_after = [&](const Segment& x) {
+    const int at = x.cost + x.n + unit_cost;
+    if (at >= c_end) {
+      Segment none = x;
+      none.j0 = none.j1 = 0;
+      return none;
     }
-    const int kvh = rel / n;
-    const int j0 = rel - kvh * n, j1 = min(n, j0 + (g1 - t));
-    const int T = seq_T(s), c = seq_c(s), l_ctx = T - c, R = c * g;
-    const int kend = min(T, j1 * kTile);
+    int b = x.b, kvh = x.kvh + 1;
+    if (kvh == Hkv) {
+      kvh = 0;
+      do ++b;
+      while (tiles_of(uniform(seqs[b])) == 0);   // (there is one: at < c_end)
+    }
+    return segment(b, kvh, 0, at);
+  };
+  Segment sg;
+  {
+    // the last sequence whose cost begins at or before the range's (it has tiles): a
+    // lane looks at every 16th, then 16 lanes at the ones from there on
+    const int c0 = range_start(pid);
+    const int lot = lane * (kMaxSeqs / 64);
+    const uint64_t lots = __ballot(lot < B && pref[min(lot, B - 1)] * Hkv <= c0);
+    int b = (63 - __builtin_clzll(lots)) * (kMaxSeqs / 64);
+    const int i = b + (lane & 15);
+    b += 31 - __builtin_clz((uint32_t)__ballot(lane < 16 && i < B && pref[min(i, B - 1)] * Hkv <= c0));
+    b = uniform(b);
+    const int start = uniform(pref[b]) * Hkv, n = tiles_of(uniform(seqs[b])), each = n + unit_cost;
+    const int kvh = uniform((c0 - start) / each), at = start + kvh * each;
+    const int j = cut_at(c0 - at, n);
+    sg = segment(b, kvh, j, at);
+    if (j == n) sg = segment_after(sg);
+  }
+  if (sg.j1 <= sg.j0) return;   // (an empty range)
 
-    // ---- this lane's rows: row block rb of the wave has the unit's rows
-    // 16 (NRB rg + rb) + lm
-    int tok[NRB];
-    bool valid[NRB];
-    uint64_t word[NRB];
-    u32x4 q[NP][NRB][KW];
+  // ---- 32 keys from base on: lane (lm, lg) has the lg-th quarter of the rows of
+  // keys base + lm and base + 16 + lm.
+  typedef __attribute__((ext_vector_type(KW))) uint32_t words;
+  struct Keys {
+    words k[2], v[2];
+    uint32_t ks[2], vs[2];
+  };
+  // What a wave loads next: keys from base on of a segment; with pages, those of 8
+  // of the 32 keys each, the same for the whole wave, looked up a step ahead
+  // through the scalar cache, so that a load waits for no lookup of its own.
+  struct Target {
+    int b, kvh, kend, base;
+    int page[kStep / 8];
+  };
+  const int by = kStep * KS;   // keys from a wave's step to its next
+  auto aim = [&](Target& x, const Segment& at, int base) {
+    x.b = at.b;
+    x.kvh = at.kvh;
+    x.kend = at.kend;
+    x.base = base;
+    if constexpr (PAGING != kSlab) {
+      typedef const __attribute__((address_space(4))) int32_t* const_table;
+      const const_table row = (const_table)(p.block_table + (size_t)at.b * p.pages_per_seq);
 #pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) {
-      const int row = kBlk * (NRB * rg + rb) + lm;
-      valid[rb] = row < R;
-      tok[rb] = valid[rb] ? row / g : 0;
-      const int h = kvh * g + (valid[rb] ? row - tok[rb] * g : 0);
-      word[rb] = valid[rb] && p.draft_mask ? p.draft_mask[b * p.C_max + tok[rb]] : 0;
-      const char* src = p.q + ((size_t)(b * p.C_max + tok[rb]) * p.Hq + h) * (D * kElt) + lg * (D / 4) * kElt;
+      for (int i = 0; i < kStep / 8; i += PAGING == kPages ? 2 : 1)
+        x.page[i] = row[min(base + 8 * i, at.kend - 1) >> p.page_shift];
+    }
+  };
+  // A block of 16 keys in consecutive rows is read through buffer descriptors that
+  // end with the segment's last key: rows past it read as zeros, whose scores are
+  // masked, and a lane's offsets never change.  (In pages of 8 a lane has an
+  // address of its own, and rows past the end re-read the last one.)
+  const int lane_codes = lm * (D / 2) + lg * (D / 8), lane_scale = lm * (D / 32) + (lg * (D / 4) / 32);
+  auto load = [&](Keys& x, const Target& at) {
 #pragma unroll
-      for (int w = 0; w < KW; ++w) {
-        if constexpr (ELT == kBF16) {
-          q[0][rb][w] = valid[rb] ? *reinterpret_cast<const u32x4*>(src + 16 * w) : u32x4{0u, 0u, 0u, 0u};
+    for (int h = 0; h < 2; ++h) {
+      auto page = [&](int i) { return uniform(min(max(at.page[i], 0), p.num_pages - 1)); };
+      if constexpr (PAGING == kSmallPages) {
+        const int key = min(at.base + kBlk * h + lm, at.kend - 1);
+        const size_t row = (((size_t)(lm < 8 ? page(2 * h) : page(2 * h + 1)) * Hkv + at.kvh) << 3) + (key & 7);
+        const size_t code = row * (D / 2) + lg * (D / 8), scale = row * (D / 32) + (lg * (D / 4) / 32);
+        x.k[h] = *reinterpret_cast<const words*>(p.k + code);
+        x.v[h] = *reinterpret_cast<const words*>(p.v + code);
+        x.ks[h] = (uint8_t)p.k_scales[scale];
+        x.vs[h] = (uint8_t)p.v_scales[scale];
+      } else {
+        const int key = at.base + kBlk * h;
+        const int rows = uniform(min(max(at.kend - key, 0), kBlk));   // (a scalar for the descriptors)
+        size_t row;
+        if constexpr (PAGING == kPages)
+          row = (((size_t)page(2 * h) * Hkv + at.kvh) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
+        else
+          row = ((size_t)at.b * Hkv + at.kvh) * p.S_max + key;
+        auto buffer = [&](const char* base, int row_bytes) {
+          return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base) + row * row_bytes, 0, rows * row_bytes,
+                                                   kBufferFormat);
+        };
+        const auto kb = buffer(p.k, D / 2), vb = buffer(p.v, D / 2);
+        if constexpr (KW == 4) {
+          x.k[h] = __builtin_bit_cast(words, __builtin_amdgcn_raw_buffer_load_b128(kb, lane_codes, 0, kStreaming));
+          x.v[h] = __builtin_bit_cast(words, __builtin_amdgcn_raw_buffer_load_b128(vb, lane_codes, 0, kStreaming));
         } else {
-          float x[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = 0.f;
-          if (valid[rb]) {
-            if constexpr (ELT == kF32) {
-              const f32x4 lo = *reinterpret_cast<const f32x4*>(src + 32 * w), hi = *reinterpret_cast<const f32x4*>(src + 32 * w + 16);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                x[e] = lo[e];
-                x[4 + e] = hi[e];
-              }
-            } else {
-              const f16x8 y = *reinterpret_cast<const f16x8*>(src + 16 * w);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] = (float)y[e];
-            }
-          }
-#pragma unroll
-          for (int part = 0; part < NP; ++part)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) q[part][rb][w][e] = split2(x[2 * e], x[2 * e + 1]);
+          x.k[h] = __builtin_bit_cast(words, __builtin_amdgcn_raw_buffer_load_b64(kb, lane_codes, 0, kStreaming));
+          x.v[h] = __builtin_bit_cast(words, __builtin_amdgcn_raw_buffer_load_b64(vb, lane_codes, 0, kStreaming));
         }
+        x.ks[h] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(buffer(p.k_scales, D / 32), lane_scale, 0, 0);
+        x.vs[h] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(buffer(p.v_scales, D / 32), lane_scale, 0, 0);
       }
     }
+  };
 
-    f32x4 o[NRB][DB];
-    float m_run[NRB], l_lane[NRB];
+  // ---- queries: row block rb of the wave has the unit's rows 16 (NRB rg + rb) + lm.
+  // x / g for a row 0 <= x < 128 of a unit, by a float reciprocal: exact there, as
+  // (x + 1/2) / g lies at least 1 / (2 g) from an integer
+  const float inv_g = 1.f / (float)g;
+  auto div_g = [&](int x) { return (int)(((float)x + 0.5f) * inv_g); };
+  constexpr int kRaw = D * kElt / 64;   // 16-byte pieces of a lane's quarter of a row
+  u32x4 q_raw[NRB][kRaw];
+  uint64_t word_raw[NRB];
+  // The entries of a lane: as of a key, the lg-th quarter of the row; with kCodes
+  // 16 from 16 lg on, and from 64 + 16 lg on, as the MFMA takes its 8-bit operand.
+  auto load_q = [&](const Segment& at) {
 #pragma unroll
     for (int rb = 0; rb < NRB; ++rb) {
+      // (rows past the unit's are computed as its last one and not stored)
+      const int row = min(kBlk * (NRB * rg + rb) + lm, at.c * g - 1), tok = div_g(row);
+      const char* src = p.q + ((size_t)(at.b * p.C_max + tok) * p.Hq + at.kvh * g + (row - tok * g)) * (D * kElt);
+#pragma unroll
+      for (int i = 0; i < kRaw; ++i) {
+        const int piece = CODES ? 32 * lg + 128 * (i >> 1) + 16 * (i & 1) : lg * (D / 4) * kElt + 16 * i;
+        q_raw[rb][i] = *reinterpret_cast<const u32x4*>(src + piece);
+      }
+      if (p.draft_mask) word_raw[rb] = p.draft_mask[at.b * p.C_max + tok];
+    }
+  };
+  auto entry = [&](const u32x4* raw, int e) {   // the e-th of a lane's entries
+    if constexpr (ELT == kF32) return __uint_as_float(raw[e >> 2][e & 3]);
+    else if constexpr (ELT == kF16) return (float)__builtin_bit_cast(f16x8, raw[e >> 3])[e & 7];
+    else return __uint_as_float((e & 1) ? raw[e >> 3][(e & 7) >> 1] & 0xffff0000u : raw[e >> 3][(e & 7) >> 1] << 16);
+  };
+
+  i32x8 qc[CODES ? QP : 1][CODES ? NRB : 1];    // kCodes: the parts' codes,
+  int qs[CODES ? NRB : 1];                      // and their scale bytes, one part's after the other's
+  u32x4 qb[CODES ? 1 : QP][CODES ? 1 : NRB][CODES ? 1 : KW];   // else: bfloat16 parts
+  uint64_t word[NRB];
+  int tok[NRB];
+  int l_ctx = 0, c = 0;   // of the segment being computed
+  f32x4 o[NRB][DB];
+  float m_run[NRB], m_use[NRB], l_lane[NRB];   // m_use: m_run, or 0 before any key
+
+  auto take_q = [&]() {
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) {
+      tok[rb] = div_g(min(kBlk * (NRB * rg + rb) + lm, c * g - 1));
+      word[rb] = word_raw[rb];
+      if constexpr (CODES) {
+        // Blocks of 32 entries have units of their own, the largest entry's power
+        // of two less 7: block (lg >> 1) is the first halves of lanes lg and lg ^ 1,
+        // block 2 + (lg >> 1) their second halves.  The MFMA takes the scale of block
+        // lg from lane lg.
+        float f[2][16];
+        int sb[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float most = 0.f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            f[i][e] = entry(q_raw[rb], 16 * i + e);
+            most = fmaxf(most, fabsf(f[i][e]));
+          }
+          most = fmaxf(most, __shfl_xor(most, 16));
+          sb[i] = max((int)(__float_as_uint(most) >> 23) - 7, 1 + kPartShift * (QP - 1));
+        }
+        const int far0 = __shfl_xor(sb[0], 48), far1 = __shfl_xor(sb[1], 48);
+        const int own = lg == 0 ? sb[0] : lg == 1 ? far0 : lg == 2 ? far1 : sb[1];
+        qs[rb] = 0;
+#pragma unroll
+        for (int part = 0; part < QP; ++part) {
+          qs[rb] |= (own - kPartShift * part) << (8 * part);
+          int codes[8];
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            part8(f[i], kv4::scale_of((uint32_t)(sb[i] - kPartShift * part)), part + 1 < QP, codes + 4 * i);
+          qc[part][rb] = i32x8{codes[0], codes[1], codes[2], codes[3], codes[4], codes[5], codes[6], codes[7]};
+        }
+      } else {
+#pragma unroll
+        for (int w = 0; w < KW; ++w) {
+          if constexpr (ELT == kBF16) {
+            qb[0][rb][w] = q_raw[rb][w];
+          } else {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = entry(q_raw[rb], 8 * w + e);
+#pragma unroll
+            for (int part = 0; part < QP; ++part)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) qb[part][rb][w][e] = split2(f[2 * e], f[2 * e + 1]);
+          }
+        }
+      }
       m_run[rb] = -INFINITY;
+      m_use[rb] = 0.f;
       l_lane[rb] = 0.f;
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+  };
 
-    // ---- 32 keys from base on: lane (lm, lg) has the lg-th quarter of the
-    // rows of keys base + lm and base + 16 + lm
-    struct Keys {
-      uint32_t k[2][KW], v[2][KW];
-      uint32_t ks[2], vs[2];
-    };
-    auto load = [&](Keys& x, int base) {
+  auto compute = [&](Keys& x, int base) {
+    const bool drafts = base + kStep > l_ctx;   // (the same for the whole wave) keys that not every row sees
+    // NaN blocks among the values of such keys: 0 times NaN would reach the rows
+    // that do not see them, so they are staged as zeros, and the rows that see them
+    // made NaN afterwards.  Bit 16 qd + i of nan[h]: the qd-th quarter of key 16 h + i.
+    uint64_t nan[2] = {0, 0};
+    uint32_t seen[NRB];   // (drafts) bit e: the lane's row sees its e-th key
+    if (drafts) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int key = base + kBlk * h + lm;
-        const bool in = key < kend;
-        size_t row;
-        if constexpr (PAGED) {
-          int page = 0;
-          if (in) page = p.block_table[(size_t)b * p.pages_per_seq + (key >> p.page_shift)];
-          page = min(max(page, 0), p.num_pages - 1);
-          row = (((size_t)page * Hkv + kvh) << p.page_shift) + (key & ((1 << p.page_shift) - 1));
-        } else {
-          row = ((size_t)b * Hkv + kvh) * p.S_max + key;
-        }
+        const bool bad = x.vs[h] == 255u;
+        nan[h] = __ballot(bad);
+        if (bad) {
+          x.vs[h] = 0;
 #pragma unroll
-        for (int w = 0; w < KW; ++w) {
-          x.k[h][w] = 0;
-          x.v[h][w] = 0;
-        }
-        x.ks[h] = 0;
-        x.vs[h] = 0;
-        if (in) {
-          const size_t at = row * (D / 2) + lg * (D / 8), sat = row * (D / 32) + (lg * (D / 4) / 32);
-          typedef __attribute__((ext_vector_type(KW))) uint32_t words;
-          const words kk = *reinterpret_cast<const words*>(p.k + at), vv = *reinterpret_cast<const words*>(p.v + at);
-#pragma unroll
-          for (int w = 0; w < KW; ++w) {
-            x.k[h][w] = kk[w];
-            x.v[h][w] = vv[w];
-          }
-          x.ks[h] = (uint8_t)p.k_scales[sat];
-          x.vs[h] = (uint8_t)p.v_scales[sat];
+          for (int w = 0; w < KW; ++w) x.v[h][w] = 0;
         }
       }
-    };
-
-    auto compute = [&](Keys& x, int base) {
-      // NaN blocks among the values of keys that not every row sees: 0 times
-      // NaN would reach the rows that do not, so such blocks are staged as
-      // zeros, and the rows that see them made NaN afterwards.  Bit 16 qd + i
-      // of nan[h]: the qd-th quarter of key 16 h + i.
-      uint64_t nan[2] = {0, 0};
-      uint32_t seen[NRB];   // (keys of the chunk's region) bit e: the lane's row sees its e-th key
-      if (base + kStep > l_ctx) {
+    }
+    // scores of two key blocks: S^T = K Q^T, lane (lm, lg) gets the keys
+    // 16 h + 4 lg + r of row lm
+    f32x4 sa[NRB][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const bool bad = x.vs[h] == 255u;
-          nan[h] = __ballot(bad);
-          if (bad) {
-            x.vs[h] = 0;
+    for (int h = 0; h < 2; ++h) {
+      if constexpr (CODES) {
+        // (the MFMA takes 4 registers of 4-bit codes; the other 4 have no value)
+        typedef __attribute__((ext_vector_type(8))) uint32_t u32x8;
+        const u32x4 k = x.k[h];
+        const i32x8 kc = __builtin_bit_cast(i32x8, (u32x8)__builtin_shufflevector(k, k, 0, 1, 2, 3, -1, -1, -1, -1));
 #pragma unroll
-            for (int w = 0; w < KW; ++w) x.v[h][w] = 0;
-          }
+        for (int rb = 0; rb < NRB; ++rb) {
+          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+          // (4: 4-bit codes, 0: 8-bit codes with 3 bits after the leading one; a part's
+          // scale is the part-th byte)
+          if constexpr (QP == 3)
+            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kc, qc[QP - 1][rb], acc, 4, 0, 0, x.ks[h], 2, qs[rb]);
+          acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kc, qc[CODES ? 1 : 0][rb], acc, 4, 0, 0, x.ks[h], 1, qs[rb]);
+          acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kc, qc[0][rb], acc, 4, 0, 0, x.ks[h], 0, qs[rb]);
+          sa[rb][h] = acc;
         }
-      }
-      // scores of two key blocks: S^T = K Q^T, lane (lm, lg) gets the keys
-      // 16 h + 4 lg + r of row lm
-      f32x4 sa[NRB][2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      } else {
         const float ks = kv4::scale_of(x.ks[h]);
         u32x4 kop[KW];
 #pragma unroll
@@ -263,126 +477,178 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
         for (int rb = 0; rb < NRB; ++rb) {
           f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int part = NP - 1; part >= 0; --part)
+          for (int part = QP - 1; part >= 0; --part)
 #pragma unroll
-            for (int w = 0; w < KW; ++w) acc = mfma32<kBF16>(kop[w], q[part][rb][w], acc);
+            for (int w = 0; w < KW; ++w) acc = mfma32<kBF16>(kop[w], qb[part][rb][w], acc);
           sa[rb][h] = acc;
         }
       }
-      // values as bfloat16 into the wave's stage
+    }
+    // values as bfloat16 into the wave's stage
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float vs = kv4::scale_of(x.vs[h]);
-        char* dst = stage + (kBlk * h + lm) * kPitch + lg * (D / 2);
+    for (int h = 0; h < 2; ++h) {
+      const float vs = kv4::scale_of(x.vs[h]);
+      char* dst = stage + (kBlk * h + lm) * kPitch + lg * (D / 2);
 #pragma unroll
-        for (int w = 0; w < KW; ++w)
-          *reinterpret_cast<u32x4*>(dst + 16 * w) =
-              u32x4{kv4::bf16_of<0>(x.v[h][w], vs), kv4::bf16_of<1>(x.v[h][w], vs), kv4::bf16_of<2>(x.v[h][w], vs),
-                    kv4::bf16_of<3>(x.v[h][w], vs)};
-      }
-      asm volatile("" ::: "memory");   // (LDS serves a wave's accesses in order)
-      // softmax
-      u32x4 pb[NRB][NP];
+      for (int w = 0; w < KW; ++w)
+        *reinterpret_cast<u32x4*>(dst + 16 * w) =
+            u32x4{kv4::bf16_of<0>(x.v[h][w], vs), kv4::bf16_of<1>(x.v[h][w], vs), kv4::bf16_of<2>(x.v[h][w], vs),
+                  kv4::bf16_of<3>(x.v[h][w], vs)};
+    }
+    asm volatile("" ::: "memory");   // (LDS serves a wave's accesses in order)
+    // softmax
+    u32x4 pb[NRB][PP];
 #pragma unroll
-      for (int rb = 0; rb < NRB; ++rb) {
-        float y[8];
+    for (int rb = 0; rb < NRB; ++rb) {
+      float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = sa[rb][e >> 2][e & 3];
-        if (base + kStep > l_ctx) {   // (the same for the whole wave)
-          seen[rb] = 0;
+      for (int e = 0; e < 8; ++e) y[e] = sa[rb][e >> 2][e & 3];
+      if (drafts) {
+        uint32_t see = 0;
+        const int k0 = base + 4 * lg - l_ctx;   // the first key as a draft token
+        if (p.draft_mask) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const int k = base + kBlk * (e >> 2) + 4 * lg + (e & 3) - l_ctx;   // draft key
-            const bool sees = p.draft_mask ? k < 0 || (k < c && ((word[rb] >> (k & 63)) & 1u))
-                                           : k <= tok[rb] && k < c;
-            if (sees) seen[rb] |= 1u << e;
-            else y[e] = -INFINITY;
+            const int k = k0 + kBlk * (e >> 2) + (e & 3);
+            const uint32_t bit = (uint32_t)(word[rb] >> (k & 63)) & (uint32_t)(k < c);
+            see |= (k < 0 ? 1u : bit & 1u) << e;
+          }
+        } else {
+          const int last = min(tok[rb], c - 1);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) see |= (uint32_t)(k0 + kBlk * (e >> 2) + (e & 3) <= last) << e;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = (see >> e) & 1u ? y[e] : -INFINITY;
+        seen[rb] = see;
+      }
+      // the running maximum moves only for a score that passes it by more than
+      // kLazyMax, so most steps exchange nothing between lanes
+      const float mx_lane = max8(y) * p.sl2;
+      if (__any(mx_lane > m_run[rb] + kLazyMax)) {
+        const float mx = row_max(mx_lane);
+        const bool raise = mx > m_run[rb] + kLazyMax;
+        const float m_new = raise ? mx : m_run[rb];
+        const float alpha = __builtin_amdgcn_exp2f(m_run[rb] - (m_new == -INFINITY ? 0.f : m_new));
+        l_lane[rb] *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[rb][db] *= alpha;
+        m_run[rb] = m_new;
+        m_use[rb] = m_new == -INFINITY ? 0.f : m_new;
+      }
+      float pr[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        pr[e] = __builtin_amdgcn_exp2f(fmaf(y[e], p.sl2, -m_use[rb]));
+        l_lane[rb] += pr[e];
+      }
+#pragma unroll
+      for (int part = 0; part < PP; ++part)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t u = pack_bf16x2(pr[2 * e], pr[2 * e + 1]);
+          pb[rb][part][e] = u;
+          if (part + 1 < PP) {   // what the rounding leaves is the next part's
+            pr[2 * e] -= __uint_as_float(u << 16);
+            pr[2 * e + 1] -= __uint_as_float(u & 0xffff0000u);
           }
         }
-        float mx = y[0];
+    }
+    // O^T += V^T P^T over the 32 keys: element e of a lane's operands is key
+    // 4 lg + e of the first block (e < 4) or 4 lg + e - 4 of the second
+    typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+    const char* vrow = stage + (4 * lg + (lm >> 2)) * kPitch + 8 * (lm & 3);
 #pragma unroll
-        for (int e = 1; e < 8; ++e) mx = fmaxf(mx, y[e]);
-        mx = row_max(mx) * p.sl2;
-        const bool raise = mx > m_run[rb] + kLazyMax;
-        if (__any(raise)) {
-          const float m_new = raise ? mx : m_run[rb];
-          const float alpha = __builtin_amdgcn_exp2f(m_run[rb] - (m_new == -INFINITY ? 0.f : m_new));
-          l_lane[rb] *= alpha;
+    for (int db = 0; db < DB; ++db) {
+      const i16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_i16x4*)(__attribute__((address_space(3))) char*)(vrow + 32 * db));
+      const i16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_i16x4*)(__attribute__((address_space(3))) char*)(vrow + kBlk * kPitch + 32 * db));
+      const u32x4 va = {__builtin_bit_cast(uint2, a0).x, __builtin_bit_cast(uint2, a0).y,
+                        __builtin_bit_cast(uint2, a1).x, __builtin_bit_cast(uint2, a1).y};
 #pragma unroll
-          for (int db = 0; db < DB; ++db) o[rb][db] *= alpha;
-          m_run[rb] = m_new;
-        }
-        const float m_use = m_run[rb] == -INFINITY ? 0.f : m_run[rb];
-        float pr[8];
+      for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          pr[e] = __builtin_amdgcn_exp2f(fmaf(y[e], p.sl2, -m_use));
-          l_lane[rb] += pr[e];
-        }
-        if constexpr (NP == 1) {
-          pb[rb][0] = pack_p<kBF16>(pr);
-        } else {
+        for (int part = PP - 1; part >= 0; --part) o[rb][db] = mfma32<kBF16>(va, pb[rb][part], o[rb][db]);
+    }
+    asm volatile("" ::: "memory");
+    if (nan[0] | nan[1]) {
 #pragma unroll
-          for (int part = 0; part < NP; ++part)
+      for (int rb = 0; rb < NRB; ++rb) {
+        const uint32_t own0 = (seen[rb] & 15u) << (4 * lg), own1 = (seen[rb] >> 4) << (4 * lg);
+        uint32_t hit = 0;   // bit qd: the row sees a NaN block in the qd-th quarter
 #pragma unroll
-            for (int e = 0; e < 4; ++e) pb[rb][part][e] = split2(pr[2 * e], pr[2 * e + 1]);
-        }
-      }
-      // O^T += V^T P^T over the 32 keys: element e of a lane's operands is key
-      // 4 lg + e of the first block (e < 4) or 4 lg + e - 4 of the second
-      typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-      const char* vrow = stage + (4 * lg + (lm >> 2)) * kPitch + 8 * (lm & 3);
+        for (int qd = 0; qd < 4; ++qd)
+          if (((uint32_t)(nan[0] >> (16 * qd)) & own0) | ((uint32_t)(nan[1] >> (16 * qd)) & own1)) hit |= 1u << qd;
+        hit |= (uint32_t)__shfl_xor((int)hit, 16);
+        hit |= (uint32_t)__shfl_xor((int)hit, 32);
 #pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const i16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_i16x4*)(__attribute__((address_space(3))) char*)(vrow + 32 * db));
-        const i16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_i16x4*)(__attribute__((address_space(3))) char*)(vrow + kBlk * kPitch + 32 * db));
-        const u32x4 va = {__builtin_bit_cast(uint2, a0).x, __builtin_bit_cast(uint2, a0).y,
-                          __builtin_bit_cast(uint2, a1).x, __builtin_bit_cast(uint2, a1).y};
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb)
-#pragma unroll
-          for (int part = NP - 1; part >= 0; --part) o[rb][db] = mfma32<kBF16>(va, pb[rb][part], o[rb][db]);
-      }
-      asm volatile("" ::: "memory");
-      if (nan[0] | nan[1]) {
-#pragma unroll
-        for (int rb = 0; rb < NRB; ++rb) {
-          const uint32_t own0 = (seen[rb] & 15u) << (4 * lg), own1 = (seen[rb] >> 4) << (4 * lg);
-          uint32_t hit = 0;   // bit qd: the row sees a NaN block in the qd-th quarter
-#pragma unroll
-          for (int qd = 0; qd < 4; ++qd)
-            if (((uint32_t)(nan[0] >> (16 * qd)) & own0) | ((uint32_t)(nan[1] >> (16 * qd)) & own1)) hit |= 1u << qd;
-          hit |= (uint32_t)__shfl_xor((int)hit, 16);
-          hit |= (uint32_t)__shfl_xor((int)hit, 32);
-#pragma unroll
-          for (int db = 0; db < DB; ++db)
-            if ((hit >> (db / (DB / 4))) & 1u) o[rb][db] = f32x4{NAN, NAN, NAN, NAN};
-        }
-      }
-    };
-
-    {
-      const int by = kStep * KS;
-      int base = j0 * kTile + kStep * kslot;
-      Keys x;
-      if (base < kend) load(x, base);
-      for (; base < kend; base += by) {
-        Keys y;
-        if (base + by < kend) load(y, base + by);
-        compute(x, base);
-        x = y;
+        for (int db = 0; db < DB; ++db)
+          if ((hit >> (db / (DB / 4))) & 1u) o[rb][db] = f32x4{NAN, NAN, NAN, NAN};
       }
     }
+  };
+
+  // pieces of units that other workgroups share, at most the range's first and
+  // last: the first and last range that have a piece of the unit, its index, its rows
+  int n_pieces = 0;
+  i32x4 piece[2];
+  const __amdgpu_buffer_rsrc_t ws_o_rsrc = __builtin_amdgcn_make_buffer_rsrc(p.ws_o, 0, p.ws_o_bytes, kBufferFormat);
+  const __amdgpu_buffer_rsrc_t ws_lse_rsrc =
+      __builtin_amdgcn_make_buffer_rsrc(p.ws_lse, 0, p.ws_lse_bytes, kBufferFormat);
+
+  // The loads of a step are under way while the one before is computed, across
+  // segments too: x holds the segment's first step at its start.
+  Keys x, y;
+  Target next;
+  load_q(sg);
+  {
+    Target at;   // (both lookups before the first load)
+    aim(at, sg, sg.j0 * kTile + kStep * kslot);
+    aim(next, sg, sg.j0 * kTile + kStep * kslot + by);
+    load(x, at);
+  }
+  for (;;) {
+    const Segment nx = segment_after(sg);
+    const bool more = nx.j1 > 0;
+    l_ctx = sg.T - sg.c;
+    c = sg.c;
+    take_q();
+
+    // ---- this wave's steps of the segment.  follow(): the loads after those of
+    // the step at base, and the lookup for the ones after them
+    const int first_base = kStep * kslot;   // of the next segment
+    auto follow = [&](Keys& z, int base) {
+      const bool inside = base + by < sg.kend;
+      if (!inside && more) aim(next, nx, first_base);   // (looked up late: once a segment)
+      if (inside || more) load(z, next);
+      if (base + 2 * by < sg.kend) aim(next, sg, base + 2 * by);
+      else if (!inside && more) aim(next, nx, first_base + by);
+    };
+    int base = sg.j0 * kTile + kStep * kslot;
+    if (base >= sg.kend) follow(x, base);   // (none: the segment's last tile is short)
+    while (base < sg.kend) {
+      follow(y, base);
+      compute(x, base);
+      base += by;
+      if (base >= sg.kend) {
+        x = y;
+        break;
+      }
+      follow(x, base);
+      compute(y, base);
+      base += by;
+    }
+    if (more) load_q(nx);
 
     // ---- the states of the waves that share the rows joined through LDS: each
-    // then has the O of its own d blocks
-    const bool whole = j0 == 0 && j1 == n;
-    const int slot = 2 * pid + (t - j0 > g0 ? 1 : 0);
-    const __amdgpu_buffer_rsrc_t ws_o_rsrc = __builtin_amdgcn_make_buffer_rsrc(p.ws_o, 0, p.ws_o_bytes, kBufferFormat);
-    const __amdgpu_buffer_rsrc_t ws_lse_rsrc =
-        __builtin_amdgcn_make_buffer_rsrc(p.ws_lse, 0, p.ws_lse_bytes, kBufferFormat);
+    // then has the O of its own d blocks.  All four waves' states are read, those
+    // of other rows with weight 0, so that the reads go out together.
+    const int R = sg.c * g;
+    const bool whole = sg.j0 == 0 && sg.j1 == sg.n;
+    // a range has at most one piece that begins its unit, its last segment, and one
+    // that does not, its first: slots 2 pid + 1 and 2 pid
+    const int slot = 2 * pid + (sg.j0 == 0 ? 1 : 0);
 #pragma unroll
     for (int rb = 0; rb < NRB; ++rb) {
       const float l_row = row_sum(l_lane[rb]);
@@ -394,84 +660,152 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
 #pragma unroll
     for (int rb = 0; rb < NRB; ++rb) {
       f32x4* own = reinterpret_cast<f32x4*>(stage) + lane;
-      if (rb) __syncthreads();   // (the last row block's reads)
+      if (rb) lds_barrier();   // (the last row block's reads)
 #pragma unroll
       for (int db = 0; db < DB; ++db) own[db * 64] = o[rb][db];
-      __syncthreads();
-      float M = -INFINITY, L = 0.f, wk[kGroupWaves];
-      for (int k = 0; k < KS; ++k) M = fmaxf(M, mst[k * RG + rg][rb][0][lm]);
-      const float Mu = M == -INFINITY ? 0.f : M;
+      lds_barrier();
+      float mk[kGroupWaves], lk[kGroupWaves];
 #pragma unroll
       for (int k = 0; k < kGroupWaves; ++k) {
-        wk[k] = 0.f;
-        if (k < KS) {
-          wk[k] = __builtin_amdgcn_exp2f(mst[k * RG + rg][rb][0][lm] - Mu);
-          L += mst[k * RG + rg][rb][1][lm] * wk[k];
-        }
+        mk[k] = mst[k][rb][0][lm];
+        lk[k] = mst[k][rb][1][lm];
+      }
+      float M = -INFINITY, L = 0.f;
+#pragma unroll
+      for (int k = 0; k < kGroupWaves; ++k) {
+        mk[k] = (k & (RG - 1)) == rg ? mk[k] : -INFINITY;
+        M = fmaxf(M, mk[k]);
+      }
+      const float Mu = M == -INFINITY ? 0.f : M;
+      float wk[kGroupWaves];
+#pragma unroll
+      for (int k = 0; k < kGroupWaves; ++k) {
+        wk[k] = __builtin_amdgcn_exp2f(mk[k] - Mu);
+        L += (k & (RG - 1)) == rg ? lk[k] * wk[k] : 0.f;
       }
       const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;   // (a NaN stays)
-      const float lse = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
       const int row = kBlk * (NRB * rg + rb) + lm;
-      const size_t orow = (size_t)(b * p.C_max + tok[rb]) * p.Hq + kvh * g + (row - tok[rb] * g);
-      if (valid[rb] && kslot == 0 && lg == 0) {
+      const bool valid = row < R;
+      const size_t orow = (size_t)(sg.b * p.C_max + tok[rb]) * p.Hq + sg.kvh * g + (row - tok[rb] * g);
+      if (valid && kslot == 0 && lg == 0) {
+        const float lse = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
         if (whole) p.lse[orow] = lse;
         else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(int, lse), ws_lse_rsrc, (slot * p.Rcap + row) * 4, 0,
                                                    kDeviceCoherent);
       }
-      for (int db = kslot; db < DB; db += KS) {
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+      constexpr int kAhead = DB / kGroupWaves;   // d blocks whose reads go out together: a quarter of them
+      for (int d0 = kslot * kAhead; d0 < DB; d0 += KS * kAhead) {
+        f32x4 part[kAhead][kGroupWaves];
 #pragma unroll
-        for (int k = 0; k < kGroupWaves; ++k)
-          if (k < KS)
-            x = add_weighted(x, wk[k], reinterpret_cast<const f32x4*>(smem + (k * RG + rg) * kStage)[db * 64 + lane]);
-        x *= inv;
-        if (!valid[rb]) continue;
-        if (whole)
-          store_out<false, ELT>(p, orow * D + 16 * db + 4 * lg, x);
-        else
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, x), ws_o_rsrc,
-                                                 ((slot * p.Rcap + row) * D + 16 * db + 4 * lg) * 4, 0, kDeviceCoherent);
-      }
-    }
-    if (!whole) {
-      // ---- count the piece once all its stores are out; the last to arrive
-      // merges the unit's pieces, in their order
-      const int first = t - j0, qf = owner(first), ql = owner(first + n - 1);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (tid == 0) {
-        int* counter = p.counters + b * Hkv + kvh;
-        const int last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == ql - qf;
-        if (last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next call
-        sh_flag = last;
-      }
-      __syncthreads();
-      if (sh_flag) {
-        const int f_slot = 2 * qf + (first > (int)(N * qf / P) ? 1 : 0);
-        for (int idx = tid; idx < R * (D / 4); idx += kGroupThreads) {
-          const int row = idx / (D / 4), d = 4 * (idx - row * (D / 4));
-          float m = -INFINITY, z = 0.f;
-          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-          for (int qq = qf; qq <= ql; ++qq) {
-            const int at = (qq == qf ? f_slot : 2 * qq) * p.Rcap + row;
-            const float lse = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(ws_lse_rsrc, at * 4, 0, kDeviceCoherent));
-            const f32x4 x = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(ws_o_rsrc, (at * D + d) * 4, 0,
-                                                                                           kDeviceCoherent));
-            const float nm = fmaxf(m, lse), nu = nm == -INFINITY ? 0.f : nm;
-            const float a = exp_diff(m, nu), w = exp_diff(lse, nu);
-            z = z * a + w;
-            acc *= a;
-            acc = add_weighted(acc, w, x);
-            m = nm;
-          }
-          const size_t orow = (size_t)(b * p.C_max + row / g) * p.Hq + kvh * g + row % g;
-          store_out<false, ELT>(p, orow * D + d, acc * (z > 0.f ? 1.f / z : z == 0.f ? 0.f : z));
-          if (d == 0) p.lse[orow] = z == 0.f ? -INFINITY : m + logf(z);
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+          for (int k = 0; k < kGroupWaves; ++k)
+            part[u][k] = reinterpret_cast<const f32x4*>(smem + k * kStage)[(d0 + u) * 64 + lane];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          f32x4 r = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < kGroupWaves; ++k)   // (other rows' values are left out, NaN and all)
+            r = (k & (RG - 1)) == rg ? add_weighted(r, wk[k], part[u][k]) : r;
+          r *= inv;
+          if (!valid) continue;
+          const int d = 16 * (d0 + u) + 4 * lg;
+          if (whole)
+            store_out<false, ELT>(p, orow * D + d, r);
+          else
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, r), ws_o_rsrc,
+                                                   ((slot * p.Rcap + row) * D + d) * 4, 0, kDeviceCoherent);
         }
       }
     }
-    __syncthreads();   // (stages, statistics and the flag are free again)
-    t += j1 - j0;
+    if (!whole) {
+      const int qf = owner(sg.cost + most_first(sg.n)), ql = owner(sg.cost + most_last(sg.n));
+      piece[n_pieces++ ? 1 : 0] = i32x4{qf, ql, sg.b * Hkv + sg.kvh, R};
+    }
+    if (!more) break;
+    lds_barrier();   // (stages and statistics are free again)
+    sg = nx;
+  }
+  if (n_pieces == 0) return;
+
+  // ---- the pieces counted on their units' counters once their stores are out; the
+  // last one of a unit to arrive merges all of them, in their order
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  lds_barrier();
+  if (lane == 0 && wave < n_pieces) {
+    const i32x4 e = wave == 0 ? piece[0] : piece[1];
+    int* counter = p.counters + e[2];
+    const int last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == e[1] - e[0];
+    if (last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next call
+    sh_last[wave] = last;
+  }
+  lds_barrier();
+  // the (row, 4 d) items of the units to merge form one list, and a thread takes
+  // kItems of them at a time, all their pieces' loads before the first is used
+  const bool m0 = uniform(sh_last[0]), m1 = n_pieces > 1 && uniform(sh_last[1]);
+  const int n0 = m0 ? uniform(piece[0][3]) * (D / 4) : 0, n1 = m1 ? uniform(piece[1][3]) * (D / 4) : 0;
+  const int pieces = max(m0 ? piece[0][1] - piece[0][0] : -1, m1 ? piece[1][1] - piece[1][0] : -1) + 1;   // of the larger
+  constexpr int kItems = 3, kBatch = 4;
+  for (int base = tid; base < n0 + n1; base += kItems * kGroupThreads) {
+    float m[kItems], z[kItems];
+    f32x4 acc[kItems];
+    int row[kItems], qf[kItems], ql[kItems], d[kItems], unit[kItems];
+#pragma unroll
+    for (int it = 0; it < kItems; ++it) {
+      const int idx = base + it * kGroupThreads;
+      const bool in0 = idx < n0;
+      const int local = in0 ? idx : idx - n0;
+      row[it] = local / (D / 4);
+      d[it] = 4 * (local - row[it] * (D / 4));
+      qf[it] = in0 ? piece[0][0] : piece[1][0];
+      ql[it] = idx < n0 + n1 ? (in0 ? piece[0][1] : piece[1][1]) : -1;   // (none for a thread past the items)
+      unit[it] = in0 ? piece[0][2] : piece[1][2];
+      m[it] = -INFINITY;
+      z[it] = 0.f;
+      acc[it] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int k0 = 0; k0 < pieces; k0 += kBatch) {
+      float lse[kItems][kBatch];
+      f32x4 part[kItems][kBatch];
+#pragma unroll
+      for (int it = 0; it < kItems; ++it)
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          lse[it][u] = -INFINITY;
+          part[it][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+          const int r = qf[it] + k0 + u;
+          if (r > ql[it]) continue;
+          const int at = (2 * r + (k0 + u == 0 ? 1 : 0)) * p.Rcap + row[it];
+          lse[it][u] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(ws_lse_rsrc, at * 4, 0, kDeviceCoherent));
+          part[it][u] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(ws_o_rsrc, (at * D + d[it]) * 4, 0,
+                                                                                        kDeviceCoherent));
+        }
+#pragma unroll
+      for (int it = 0; it < kItems; ++it) {
+        float nm = m[it];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) nm = fmaxf(nm, lse[it][u]);
+        const float nu = nm == -INFINITY ? 0.f : nm;
+        const float a = exp_diff(m[it], nu);
+        z[it] *= a;
+        acc[it] *= a;
+        m[it] = nm;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const float w = exp_diff(lse[it][u], nu);
+          z[it] += w;
+          acc[it] = add_weighted(acc[it], w, part[it][u]);
+        }
+      }
+    }
+#pragma unroll
+    for (int it = 0; it < kItems; ++it) {
+      if (base + it * kGroupThreads >= n0 + n1) continue;
+      const int b = unit[it] / Hkv, kvh = unit[it] - b * Hkv, tk = div_g(row[it]);
+      const size_t orow = (size_t)(b * p.C_max + tk) * p.Hq + kvh * g + (row[it] - tk * g);
+      store_out<false, ELT>(p, orow * D + d[it], acc[it] * (z[it] > 0.f ? 1.f / z[it] : z[it] == 0.f ? 0.f : z[it]));
+      if (d[it] == 0) p.lse[orow] = z[it] == 0.f ? -INFINITY : m[it] + logf(z[it]);
+    }
   }
 }
 
@@ -484,14 +818,14 @@ specmoe_verify_desc sized(const specmoe_verify_desc* d) {
   return x;
 }
 
-template <int ELT, int D, bool PAGED>
+template <int ELT, int D, int PAGING>
 void launch_kv4(const Kv4Params& p, hipStream_t stream) {
   constexpr int kElt = ELT == kF32 ? 4 : 2;
   for (int b0 = 0; b0 < p.B; b0 += kMaxSeqs) {   // (as specmoe_verify_attn: consecutive launches)
     Kv4Params s = p;
     s.B = p.B - b0 < kMaxSeqs ? p.B - b0 : kMaxSeqs;
     s.q = p.q + (size_t)b0 * p.C_max * p.Hq * D * kElt;
-    if (PAGED) {
+    if (PAGING != kSlab) {
       s.block_table = p.block_table + (size_t)b0 * p.pages_per_seq;
     } else {
       const size_t rows = (size_t)b0 * p.Hkv * p.S_max;
@@ -507,20 +841,22 @@ void launch_kv4(const Kv4Params& p, hipStream_t stream) {
     s.lse = p.lse + (size_t)b0 * p.C_max * p.Hq;
     const int blocks = (p.Rcap + kBlk - 1) / kBlk;
     s.row_groups = blocks <= 2 ? 1 : blocks <= 4 ? 2 : 4;
-    if (blocks == 1) hipLaunchKernelGGL((kv4_attn_kernel<ELT, D, PAGED, 1>), dim3(p.P), dim3(kGroupThreads), 0, stream, s);
-    else hipLaunchKernelGGL((kv4_attn_kernel<ELT, D, PAGED, 2>), dim3(p.P), dim3(kGroupThreads), 0, stream, s);
+    if (blocks == 1) hipLaunchKernelGGL((kv4_attn_kernel<ELT, D, PAGING, 1>), dim3(p.P), dim3(kGroupThreads), 0, stream, s);
+    else hipLaunchKernelGGL((kv4_attn_kernel<ELT, D, PAGING, 2>), dim3(p.P), dim3(kGroupThreads), 0, stream, s);
   }
+}
+
+template <int ELT, int D>
+void launch_kv4_paging(const Kv4Params& p, hipStream_t s) {
+  if (!p.block_table) launch_kv4<ELT, D, kSlab>(p, s);
+  else if (p.page_shift >= 4) launch_kv4<ELT, D, kPages>(p, s);
+  else launch_kv4<ELT, D, kSmallPages>(p, s);
 }
 
 template <int ELT>
 void launch_kv4_for(int D, const Kv4Params& p, hipStream_t s) {
-  if (D == 128) {
-    if (p.block_table) launch_kv4<ELT, 128, true>(p, s);
-    else launch_kv4<ELT, 128, false>(p, s);
-  } else {
-    if (p.block_table) launch_kv4<ELT, 64, true>(p, s);
-    else launch_kv4<ELT, 64, false>(p, s);
-  }
+  if (D == 128) launch_kv4_paging<ELT, 128>(p, s);
+  else launch_kv4_paging<ELT, 64>(p, s);
 }
 
 }  // namespace
@@ -543,7 +879,7 @@ int specmoe_verify_attn_kv4(const void* q, const specmoe_kv4* cache, const int32
   if (desc->flags != 0) return SPECMOE_ERR_FLAGS;
   if (block_table && !paged) return SPECMOE_ERR_NULL_POINTER;
   // (tiles here hold 128 keys whatever the type)
-  if ((int64_t)kMaxSeqs * desc->Hkv * ((desc->S_max + (int64_t)kTile - 1) / kTile) >= ((int64_t)1 << 31))
+  if ((int64_t)kMaxSeqs * desc->Hkv * ((desc->S_max + (int64_t)kTile - 1) / kTile + kUnitCost) >= ((int64_t)1 << 31))
     return SPECMOE_ERR_SHAPE;
   const specmoe_verify_desc d = sized(desc);
   st = validate_desc(&d);
