@@ -18,7 +18,7 @@ constexpr int kTile = 128;            // keys of a tile
 constexpr int kStep = 32;             // keys that a wave takes at a time: two MFMA blocks
 // The schedule (see the kernel): tiles a workgroup from which on units cost and cuts
 // snap, what a unit costs beside its tiles, and how near a unit's end a cut goes to it
-constexpr int kManyTiles = 6, kUnitCost = 2, kSnap = 2;
+constexpr int kManyTiles = 6, kUnitCost = 4, kSnap = 3;
 
 // Where the cache's rows are: a slab per sequence, or pages of at least 16 tokens (a
 // block of 16 keys is in one page), or of 8
@@ -598,7 +598,9 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
       __builtin_amdgcn_make_buffer_rsrc(p.ws_lse, 0, p.ws_lse_bytes, kBufferFormat);
 
   // The loads of a step are under way while the one before is computed, across
-  // segments too: x holds the segment's first step at its start.
+  // segments too: y holds the segment's first step at its start.  (One copy of the
+  // step's code, with 20 moves to a step: two copies without moves take longer, 38.4
+  // against 35.9 us for 64 sequences, 145 against 141 for long ones.)
   Keys x, y;
   Target next;
   load_q(sg);
@@ -606,7 +608,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
     Target at;   // (both lookups before the first load)
     aim(at, sg, sg.j0 * kTile + kStep * kslot);
     aim(next, sg, sg.j0 * kTile + kStep * kslot + by);
-    load(x, at);
+    load(y, at);
   }
   for (;;) {
     const Segment nx = segment_after(sg);
@@ -626,18 +628,11 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
       else if (!inside && more) aim(next, nx, first_base + by);
     };
     int base = sg.j0 * kTile + kStep * kslot;
-    if (base >= sg.kend) follow(x, base);   // (none: the segment's last tile is short)
-    while (base < sg.kend) {
+    if (base >= sg.kend) follow(y, base);   // (none: the segment's last tile is short)
+    for (; base < sg.kend; base += by) {
+      x = y;
       follow(y, base);
       compute(x, base);
-      base += by;
-      if (base >= sg.kend) {
-        x = y;
-        break;
-      }
-      follow(x, base);
-      compute(y, base);
-      base += by;
     }
     if (more) load_q(nx);
 
@@ -839,9 +834,14 @@ void launch_kv4(const Kv4Params& p, hipStream_t stream) {
     if (p.draft_mask) s.draft_mask = p.draft_mask + (size_t)b0 * p.C_max;
     s.out = p.out + (size_t)b0 * p.C_max * p.Hq * D * kElt;
     s.lse = p.lse + (size_t)b0 * p.C_max * p.Hq;
+    // Row blocks of 16: two to a wave (the conversion of its keys and values serves
+    // both: 64 sequences, trees of 16, bf16, four blocks: 63 us; one to a wave 80),
+    // but in float32, where two do not fit the registers (8 sequences, chunks of 5,
+    // four heads: 47 us; one to a wave 18).
     const int blocks = (p.Rcap + kBlk - 1) / kBlk;
-    s.row_groups = blocks <= 2 ? 1 : blocks <= 4 ? 2 : 4;
-    if (blocks == 1) hipLaunchKernelGGL((kv4_attn_kernel<ELT, D, PAGING, 1>), dim3(p.P), dim3(kGroupThreads), 0, stream, s);
+    const bool single = blocks == 1 || (ELT == kF32 && blocks <= 4);
+    s.row_groups = single ? (blocks <= 1 ? 1 : blocks <= 2 ? 2 : 4) : blocks <= 2 ? 1 : blocks <= 4 ? 2 : 4;
+    if (single) hipLaunchKernelGGL((kv4_attn_kernel<ELT, D, PAGING, 1>), dim3(p.P), dim3(kGroupThreads), 0, stream, s);
     else hipLaunchKernelGGL((kv4_attn_kernel<ELT, D, PAGING, 2>), dim3(p.P), dim3(kGroupThreads), 0, stream, s);
   }
 }
