@@ -131,7 +131,7 @@ typedef struct specmoe_kv4_desc {
  * Asynchronous on `stream`; allocates nothing.  Errors, in this order:
  * SPECMOE_ERR_NULL_POINTER (desc), SPECMOE_ERR_DTYPE, SPECMOE_ERR_HEAD_DIM,
  * SPECMOE_ERR_SHAPE (B < 0, Hkv, N_max or S_max < 1, Hkv > 2^20,
- * B N_max >= 2^31 or B * ceil(N_max / 16) >= 2^24 - 1), SPECMOE_ERR_PAGES; then, with
+ * B N_max >= 2^31 or B * ceil(N_max / 4) >= 2^24 - 1), SPECMOE_ERR_PAGES; then, with
  * B > 0, SPECMOE_ERR_NULL_POINTER, SPECMOE_ERR_ALIGN, SPECMOE_ERR_LAUNCH.
  */
 int specmoe_read_kv4(const specmoe_kv4* cache, const int32_t* block_table, const int32_t* first, const int32_t* rows,

@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kF32 = SPECMOE_F32, kBF16 = SPECMOE_BF16, kF16 = SPECMOE_F16;
 constexpr int kMaxThreads = 512;
+constexpr int kManyTokens = 1024, kManyThreads = 256;   // (append) tokens from which on workgroups are smaller
 constexpr int kMaxDraftBits = 64;
 constexpr int64_t kMaxTokens = ((int64_t)1 << 32) / kMaxThreads - 1;
 
@@ -125,7 +126,9 @@ __global__ __launch_bounds__(kMaxThreads) void append_kv4_kernel(AppendParams p)
   constexpr int LP = D / VE / 2;     // items of a query's row: chunk pairs
   constexpr int LK = D / 8;          // items of a key's or value's row
   constexpr int kRow = D * kElt;
-  __shared__ __attribute__((aligned(16))) double turn[2][D / 2];   // cosines, sines
+  // cosines and sines, for the keys and, in fp32, for the queries
+  __shared__ __attribute__((aligned(16))) double turn[2][D / 2];
+  __shared__ __attribute__((aligned(16))) float turn_q[2][D / 2];
 
   const int tid = threadIdx.x;
   const int b = blockIdx.x / p.C_max, i = blockIdx.x - b * p.C_max;
@@ -148,6 +151,8 @@ __global__ __launch_bounds__(kMaxThreads) void append_kv4_kernel(AppendParams p)
     sincospi(2.0 * t, &sn, &cs);
     turn[0][tid] = cs;
     turn[1][tid] = sn;
+    turn_q[0][tid] = (float)cs;
+    turn_q[1][tid] = (float)sn;
   }
   const Place at = place_of(p.paging, p.Hkv, p.S_max, b, l + i);
   __syncthreads();
@@ -188,12 +193,12 @@ __global__ __launch_bounds__(kMaxThreads) void append_kv4_kernel(AppendParams p)
         }
       }
       if (turned) {
-        const double* cs = turn[0] + s * VE;
-        const double* sn = turn[1] + s * VE;
+        const float* cs = turn_q[0] + s * VE;
+        const float* sn = turn_q[1] + s * VE;
         if (!p.pairs) {
 #pragma unroll
           for (int e = 0; e < VE; ++e) {
-            const float u = a[e], w = z[e], co = (float)cs[e], si = (float)sn[e];
+            const float u = a[e], w = z[e], co = cs[e], si = sn[e];
             a[e] = u * co - w * si;
             z[e] = w * co + u * si;
           }
@@ -201,8 +206,7 @@ __global__ __launch_bounds__(kMaxThreads) void append_kv4_kernel(AppendParams p)
 #pragma unroll
           for (int e = 0; e < VE; e += 2) {
             const float u = a[e], w = a[e + 1], y = z[e], x = z[e + 1];
-            const float c0 = (float)cs[e / 2], s0 = (float)sn[e / 2];
-            const float c1 = (float)cs[VE / 2 + e / 2], s1 = (float)sn[VE / 2 + e / 2];
+            const float c0 = cs[e / 2], s0 = sn[e / 2], c1 = cs[VE / 2 + e / 2], s1 = sn[VE / 2 + e / 2];
             a[e] = u * c0 - w * s0;
             a[e + 1] = w * c0 + u * s0;
             z[e] = y * c1 - x * s1;
@@ -291,7 +295,7 @@ __global__ __launch_bounds__(kMaxThreads) void append_kv4_kernel(AppendParams p)
 // --------------------------------------------------------------------- read
 
 constexpr int kReadThreads = 256;
-constexpr int kReadTokens = 16;   // tokens of a workgroup
+constexpr int kReadTokens = 4;   // tokens of a workgroup (16 to 500 rows each, 148 MB: 35 us, with 16 tokens 41)
 
 struct ReadParams {
   kv4::Cache cache;
@@ -473,7 +477,11 @@ template <int ELT>
 void launch_append(int D, const AppendParams& p, unsigned tokens, hipStream_t s) {
   const int LP = D * (ELT == kF32 ? 4 : 2) / 32;
   const int64_t items = ((p.Hq * LP + 63) & ~63) + 2 * p.Hkv * (D / 8);
-  const int64_t rounds = (items + kMaxThreads - 1) / kMaxThreads;
+  // A prompt's tokens in several rounds of fewer waves, as more tokens to a CU hide
+  // more (prompts of 8, 9,700 tokens, 55 us against 67); a few tokens in one round
+  // (one token 3.6 us against 4.2).
+  const int most = tokens > kManyTokens ? kManyThreads : kMaxThreads;
+  const int64_t rounds = (items + most - 1) / most;
   const int threads = (int)(((items + rounds - 1) / rounds + 63) / 64 * 64);
   if (D == 128) hipLaunchKernelGGL((append_kv4_kernel<ELT, 128>), dim3(tokens), dim3(threads), 0, s, p);
   else hipLaunchKernelGGL((append_kv4_kernel<ELT, 64>), dim3(tokens), dim3(threads), 0, s, p);
