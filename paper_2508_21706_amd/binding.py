@@ -914,10 +914,15 @@ def _kv4(cache: KV4Cache, B: int, block_table: Optional[torch.Tensor], gpu: int)
     n, Hkv, rows, half = kc.shape
     codes, scales = (n, Hkv, rows, half), (n, Hkv, rows, half // 16)
     u8 = torch.uint8
-    _check_on(kc, "k_codes", codes, u8, gpu)
-    _check_on(ks, "k_scales", scales, u8, gpu)
-    _check_on(vc, "v_codes", codes, u8, gpu)
-    _check_on(vs, "v_scales", scales, u8, gpu)
+    if not (kc.shape == vc.shape == codes and ks.shape == vs.shape == scales
+            and kc.dtype is ks.dtype is vc.dtype is vs.dtype is u8
+            and kc.get_device() == ks.get_device() == vc.get_device() == vs.get_device() == gpu
+            and kc.is_contiguous() and ks.is_contiguous() and vc.is_contiguous() and vs.is_contiguous()):
+        # (one check for all; the tensor that fails it is named here)
+        _check_on(kc, "k_codes", codes, u8, gpu)
+        _check_on(ks, "k_scales", scales, u8, gpu)
+        _check_on(vc, "v_codes", codes, u8, gpu)
+        _check_on(vs, "v_scales", scales, u8, gpu)
     ptrs = KV4(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr())
     if block_table is None:
         if n != B:

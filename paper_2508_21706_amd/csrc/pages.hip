@@ -21,7 +21,7 @@ constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kSlotThreads = 256;
 // Slots up to which the step's workgroup writes them itself
-constexpr int64_t kOwnSlots = 16384;
+constexpr int64_t kOwnSlots = 2048;
 
 struct Params {
   const int32_t* ctx_lens;
@@ -77,62 +77,40 @@ __device__ int block_scan(int x, int* sums, int* waves, int& total) {
   return x + before;
 }
 
-// The first thread whose inclusive sum exceeds i (i < total)
-__device__ __forceinline__ int owner_of(const int* sums, int i) {
-  int lo = 0;
-#pragma unroll
-  for (int step = kThreads / 2; step; step >>= 1) lo += sums[lo + step - 1] <= i ? step : 0;
-  return lo;
-}
-
-// Copies the pages that the requests of this lot give back or take: sums[] the
-// inclusive sums of their numbers, n: the first n of all of them; place(r, k, i, from,
-// to): where request r's k-th page, the i-th of all, is and goes.
+// Copies the first n of the pages that this lot's requests give back or take, a page to
+// a thread, which searches for its request in the inclusive sums: place(r, k, i, from,
+// to) is where request r's k-th page, the i-th of all, is and goes.
 //
-// A few pages in all are one list, a page to a thread, which searches for its request.
-// Many go request by request, eight of them to a wave at a time, whose loads are out
-// before the first store (the searches of 17,000 pages take 19 us, the requests 8;
-// with one page for every tenth of 1024 requests 6 and 12).
-constexpr int kListPages = 2 * kThreads;
-template <class Place>
-__device__ __forceinline__ void copy_pages(const int* sums, int n, const Place& place) {
-  const int tid = threadIdx.x;
-  if (n <= kListPages) {
-    for (int i = tid; i < n; i += kThreads) {
-      const int r = owner_of(sums, i);
-      const int32_t* from;
-      int32_t* to;
-      place(r, i - (r ? sums[r - 1] : 0), i, from, to);
-      *to = *from;
-    }
-    return;
-  }
-  constexpr int kTogether = 8;
-  const int wave = tid >> 6, lane = tid & 63;
-  for (int r0 = wave; r0 < kThreads; r0 += kTogether * kWaves) {
-    int at[kTogether], count[kTogether], most = 0;
+// A search is ten dependent LDS reads and the page a load behind them; kTogether of both
+// are in flight.
+template <int kTogether, class Place>
+__device__ __forceinline__ void copy_list(const int* sums, int n, const Place& place) {
+  for (int i0 = threadIdx.x; i0 < n; i0 += kTogether * kThreads) {
+    int at[kTogether], lo[kTogether];
+#pragma unroll
+    for (int u = 0; u < kTogether; ++u) at[u] = min(i0 + u * kThreads, n - 1), lo[u] = 0;
+    // the first thread whose inclusive sum exceeds the item's index
+#pragma unroll
+    for (int step = kThreads / 2; step; step >>= 1)
+#pragma unroll
+      for (int u = 0; u < kTogether; ++u) lo[u] += sums[lo[u] + step - 1] <= at[u] ? step : 0;
+    int32_t* to[kTogether];
+    int32_t x[kTogether];
 #pragma unroll
     for (int u = 0; u < kTogether; ++u) {
-      const int r = r0 + u * kWaves;
-      at[u] = r ? sums[r - 1] : 0;
-      count[u] = min(sums[r], n) - at[u];
-      most = max(most, count[u]);
+      const int32_t* from;
+      place(lo[u], at[u] - (lo[u] ? sums[lo[u] - 1] : 0), at[u], from, to[u]);
+      x[u] = *from;
     }
-    for (int k = lane; k - lane < most; k += 64) {
-      const int32_t* from[kTogether];
-      int32_t* to[kTogether];
-      int32_t x[kTogether];
+    // (past the end the last page is written again, with the same value)
 #pragma unroll
-      for (int u = 0; u < kTogether; ++u)
-        if (k < count[u]) {
-          place(r0 + u * kWaves, k, at[u] + k, from[u], to[u]);
-          x[u] = *from[u];
-        }
-#pragma unroll
-      for (int u = 0; u < kTogether; ++u)
-        if (k < count[u]) *to[u] = x[u];
-    }
+    for (int u = 0; u < kTogether; ++u) *to[u] = x[u];
   }
+}
+template <class Place>
+__device__ __forceinline__ void copy_pages(const int* sums, int n, const Place& place) {
+  if (n <= kThreads) copy_list<1>(sums, n, place);
+  else copy_list<4>(sums, n, place);
 }
 
 __device__ __forceinline__ int64_t slot_of(const Params& p, int b, const Need& n, int held, int i) {
