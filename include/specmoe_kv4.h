@@ -79,8 +79,12 @@ int specmoe_append_kv4(const void* q, const void* k, const void* v, const void* 
  *   desc         as in specmoe_verify_attn; dtype is the type of q and out.
  *                grid_blocks 0: 512 workgroups, two per CU.
  *
- * Queries are taken exactly; the codes' products with them are summed in fp32,
- * and so are the statistics of the softmax.  For their product with the values,
+ * The codes' products with the queries are summed in fp32, and so are the
+ * statistics of the softmax.  Queries are taken exactly, but for entries under
+ * 2^-13 of the largest of their block of 32 in a 16-bit type with D = 128: such
+ * an entry is off by at most 2^-22 (bfloat16) or 2^-27 (float16) of that largest
+ * one.  A query that holds an infinity or NaN, or
+ * whose product with a key it sees passes float32's range, gets NaN.  For their product with the values,
  * probabilities are rounded to bfloat16 when dtype is bfloat16, and kept to 16
  * bits for float16 and 24 for float32.  Padding rows and tokens that see no key
  * get out = 0 and lse = -inf.  Keys that a token does not see leave its results

@@ -6,8 +6,12 @@ Rows past a sequence's last key hold NaN blocks, and table entries past its page
 a page of them, so what must not be read shows.
 
 Tolerances, per row, with h = eps / 2 of the type: a score is off by at most
-ds = 2^-24 (D + 8) A, A the largest scale sum |q k| of the row (the dot product's
-roundings; queries and codes are exact), a probability by ds + 2^-21 more (the
+ds = 2^-24 (D + 8) A + dq, A the largest scale sum |q k| of the row (the dot product's
+roundings; codes are exact) and dq what the queries' 8-bit parts leave (of bfloat16
+and float16 with D = 128): at most half a step, 2^-10, of the last part's unit, which
+is 2^-5 per part under the first's, of which the block's largest entry is at least 2^7.
+That is 2^-22 (two parts) and 2^-27 (three) of the largest |q| of the block, times the
+sum of the block's |k|.  A probability is off by ds + 2^-21 more (the
 exponential and its argument) and by hp, its rounding for the product with the values:
 2^-8 of bfloat16's, cut to 16 bits for float16 (2^-15) and to 24 for float32 (2^-23);
 sums add (T / 4 + 64) 2^-24.  So with W = sum p |v|
@@ -27,6 +31,7 @@ from test_gpu_parity import dev, note
 pytestmark = pytest.mark.gpu
 
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+DQ = {"f32": 0.0, "bf16": 2.0 ** -22, "f16": 2.0 ** -27}
 HP = {"f32": 2.0 ** -23, "bf16": 2.0 ** -8, "f16": 2.0 ** -15}
 GRID = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
 
@@ -116,10 +121,10 @@ def check(x, out, lse, label="", rows=None, skip=()):
         T = l + c
         k, v = (decode_ref(x["slab"][n][b, :, :T], x["slab"][n + 1][b, :, :T]) for n in (0, 2))
         for i in range(c):
-            if (b, i) in skip:
-                continue
             sees = sees_of(x, b, i)
             for head in range(Hq):
+                if (b, i, head) in skip:
+                    continue
                 kk, vv = k[head // g], v[head // g]
                 ref_o, ref_l = scored_row_ref(q[b, i, head], np.where(sees[:, None], kk, 0), np.where(sees[:, None], vv, 0),
                                               x["scale"], sees)
@@ -131,6 +136,9 @@ def check(x, out, lse, label="", rows=None, skip=()):
                 p = np.exp(sc - ref_l)
                 W = p @ np.abs(vv[sees])
                 ds = 2.0 ** -24 * (D + 8) * A
+                if D == 128:
+                    per_block = np.abs(kk[sees]).reshape(-1, 4, 32).sum(-1) @ np.abs(q[b, i, head]).reshape(4, 32).max(-1)
+                    ds += DQ[x["dtype"]] * float(per_block.max()) * x["scale"]
                 rel = ds + 2.0 ** -21 + (T / 4 + 64) * 2.0 ** -24
                 tol_o = (2 * rel + hp) * W + h * np.abs(ref_o) * (1 + h) + 2.0 ** -24 * (x["dtype"] == "f16")
                 tol_l = rel + 2.0 ** -23 * abs(ref_l)
@@ -195,6 +203,38 @@ def test_results_do_not_depend_on_timing():
 def test_large_scores():
     x = make(7, "bf16", [200, 33], [2, 3], C=3, q_scale=30.0)
     check(x, *call(x), label="large scores")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_queries_of_very_unlike_entries(dtype, D):
+    """A large entry in every block, against keys that are 0 there: the small ones, down
+    to 2^-20 of it, make the scores."""
+    x = make(17, dtype, [150, 40], [3, 2], C=3, D=D, Hq=4, q_scale=2.0 ** -3)
+    gen = torch.Generator().manual_seed(17)
+    q = x["q"].float() * torch.exp2(-torch.randint(0, 8, x["q"].shape, generator=gen).float())
+    for at, size in ((3, 2.0 ** 9), (16, 1.5 * 2.0 ** 8), (31, 448.0)):
+        q[..., at::32] = q[..., at::32].sign() * size
+        x["slab"][0][..., at // 2::16] &= 0x0F if at % 2 else 0xF0
+    x["q"] = q.to(TYPES[dtype])
+    check(x, *call(x), label=f"unlike entries {dtype} {D}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_queries_at_their_types_ends(dtype):
+    """Entries up to the largest finite one, and subnormal ones, in rows of their own.
+
+    Dot products are summed in float32: of bfloat16 entries up to 2^128, 128 products
+    with keys up to 3 pass its largest, 2^128, so those rows (head 0 and 1 of the first
+    tokens) are not compared; a 2^-10th of them sums to 2^128 2^-10 128 3 at most, and is."""
+    x = make(18, dtype, [150, 40], [3, 2], C=3, Hq=4)
+    info = torch.finfo(TYPES[dtype])
+    x["q"][:, 0, :2] = (x["q"][:, 0, :2].float().clamp(-1, 1) * info.max).to(TYPES[dtype])
+    x["q"][:, 0, 2:] = (x["q"][:, 0, 2:].float().clamp(-1, 1) * info.max * 2.0 ** -10).to(TYPES[dtype])
+    x["q"][:, 1, 1] = (x["q"][:, 1, 1].float() * info.tiny / 4).to(TYPES[dtype])
+    # (scores within float32, and not all of them past a softmax's reach)
+    x["scale"] = 2.0 ** -120 if dtype == "bf16" else 2.0 ** -12
+    check(x, *call(x), label=f"ends {dtype}", skip=[(b, 0, h) for b in (0, 1) for h in (0, 1)] if dtype == "bf16" else ())
 
 
 def test_exponents_at_their_ends():
