@@ -558,19 +558,35 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
     // 4 lg + e of the first block (e < 4) or 4 lg + e - 4 of the second
     typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
     const char* vrow = stage + (4 * lg + (lm >> 2)) * kPitch + 8 * (lm & 3);
-#pragma unroll
-    for (int db = 0; db < DB; ++db) {
+    auto read_v = [&](int db) {
       const i16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
           (lds_i16x4*)(__attribute__((address_space(3))) char*)(vrow + 32 * db));
       const i16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
           (lds_i16x4*)(__attribute__((address_space(3))) char*)(vrow + kBlk * kPitch + 32 * db));
-      const u32x4 va = {__builtin_bit_cast(uint2, a0).x, __builtin_bit_cast(uint2, a0).y,
-                        __builtin_bit_cast(uint2, a1).x, __builtin_bit_cast(uint2, a1).y};
+      return u32x4{__builtin_bit_cast(uint2, a0).x, __builtin_bit_cast(uint2, a0).y, __builtin_bit_cast(uint2, a1).x,
+                   __builtin_bit_cast(uint2, a1).y};
+    };
+    // The reads of kAheadV d blocks are under way: left to itself the compiler waits for
+    // each before its products (64 sequences, chunks of 5: 37.0 against 34.8 us, trees of
+    // 16 in float16 70.3 against 68.5).
+    constexpr int kAheadV = PP == 1 ? 4 : 3;
+    u32x4 va[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) va[db] = read_v(db);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
-        for (int part = PP - 1; part >= 0; --part) o[rb][db] = mfma32<kBF16>(va, pb[rb][part], o[rb][db]);
+        for (int part = PP - 1; part >= 0; --part) o[rb][db] = mfma32<kBF16>(va[db], pb[rb][part], o[rb][db]);
+    constexpr int kMfma = 0x8, kLdsRead = 0x100;
+    __builtin_amdgcn_sched_group_barrier(kLdsRead, 2 * kAheadV, 0);
+#pragma unroll
+    for (int db = kAheadV; db < DB; ++db) {
+      __builtin_amdgcn_sched_group_barrier(kMfma, NRB * PP, 0);
+      __builtin_amdgcn_sched_group_barrier(kLdsRead, 2, 0);
     }
+    __builtin_amdgcn_sched_group_barrier(kMfma, NRB * PP * kAheadV, 0);
     asm volatile("" ::: "memory");
     if (nan[0] | nan[1]) {
 #pragma unroll
