@@ -1049,6 +1049,8 @@ def verify_attn_kv4(q: torch.Tensor, cache: KV4Cache, ctx_lens: torch.Tensor, ch
         lse = _empty((B, C_max, Hq), torch.float32, q.device, stream)
     _check_on(out, "out", (B, C_max, Hq, D), dt, dev)
     _check_on(lse, "lse", (B, C_max, Hq), torch.float32, dev)
+    if out.data_ptr() == q.data_ptr() and q.numel():   # (workgroups that share a unit read its queries at any time)
+        raise ValueError("out must not be q's memory")
     desc = make_desc(B, Hq, Hkv, D, C_max, S_max, _dtype_code(q), grid_blocks)
     if B > 0:
         if workspace is None:

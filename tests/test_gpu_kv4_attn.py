@@ -314,6 +314,34 @@ def test_lengths_out_of_range_and_bad_pages_stay_in_bounds():
         assert torch.equal(out[b], good[0][b]) and torch.equal(lse[b], good[1][b])
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f16", 64), ("f32", 64)])
+@pytest.mark.parametrize("S", [1, 5, 37, 143])
+def test_full_slabs_of_odd_capacities(dtype, D, S):
+    """Every row of the slabs is a key, and the cache's tensors end with the last one."""
+    c = min(S, 3)
+    x = make(19, dtype, [S - c, S - 1, 0], [c, 1, c], C=c, D=D, S=S)
+    check(x, *call(x), label=f"S {S} {dtype} {D}")
+
+
+def test_sequences_that_share_their_first_pages():
+    x = make(20, "bf16", [70, 64, 40], [2, 2, 2], C=2, page=16)
+    for t in x["slab"]:
+        t[1, :, :64], t[2, :, :32] = t[0, :, :64], t[0, :, :32]
+    cache, table = on_gpu(x)
+    ref = call(x, cache, table)
+    table[1, :4], table[2, :2] = table[0, :4].clone(), table[0, :2].clone()
+    got = call(x, cache, table)
+    assert torch.equal(ref[0], got[0]) and torch.equal(ref[1], got[1])
+
+
+def test_results_in_the_queries_memory_are_refused():
+    x = make(21, "bf16", [40], [2])
+    cache, _ = on_gpu(x)
+    q, n = x["q"].to(dev()), torch.tensor([2], dtype=torch.int32, device=dev())
+    with pytest.raises(ValueError, match="q's memory"):
+        pkg.verify_attn_kv4(q, cache, n, n, x["scale"], out=q)
+
+
 def test_agrees_with_the_16_bit_path_on_rows_that_are_read_back():
     """The same call of verify_attn on the cache that read_kv4 makes."""
     x = make(14, "bf16", [600, 31], [5, 4], Hq=32, Hkv=8, C=5)
