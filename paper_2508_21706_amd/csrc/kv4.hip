@@ -29,7 +29,7 @@ namespace {
 
 constexpr int kF32 = SPECMOE_F32, kBF16 = SPECMOE_BF16, kF16 = SPECMOE_F16;
 constexpr int kMaxThreads = 512;
-constexpr int kManyTokens = 1024, kManyThreads = 256;   // (append) tokens from which on workgroups are smaller
+constexpr int kManyTokens = 1024, kManyThreads = 192;   // (append) tokens from which on workgroups are smaller
 constexpr int kMaxDraftBits = 64;
 constexpr int64_t kMaxTokens = ((int64_t)1 << 32) / kMaxThreads - 1;
 
