@@ -45,6 +45,16 @@ constexpr int kStep = 32;             // keys that a wave takes at a time: two M
 // The schedule (see the kernel): tiles a workgroup from which on units cost and cuts
 // snap, what a unit costs beside its tiles, and how near a unit's end a cut goes to it
 constexpr int kManyTiles = 6, kUnitCost = 4, kSnap = 3;
+// Pieces of a unit, about: its join is one workgroup's, a round trip for every few of
+// them (4 sequences of 23,000 keys, one KV head, chunks of 2, float16: 60 us with all
+// workgroups, 128 pieces; 33 with 32, 30 with 24; 3 sequences of 3,500 keys, 4 KV heads,
+// trees of 3 to 12: 46, 45, 53)
+constexpr int kMostPieces = 32;
+
+template <int N>
+struct Int {
+  static constexpr int value = N;
+};
 
 // Where the cache's rows are: a slab per sequence, or pages of at least 16 tokens (a
 // block of 16 keys is in one page), or of 8
@@ -53,7 +63,6 @@ constexpr int kSlab = 0, kPages = 1, kSmallPages = 2;
 struct Kv4Params : Params {   // (k and v: the codes)
   const char* k_scales;
   const char* v_scales;
-  int row_groups;   // waves of a workgroup that have different rows: 1, 2 or 4
 };
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
@@ -147,8 +156,6 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
   const int pid = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int lm = lane & 15, lg = lane >> 4;
   const int B = p.B, Hkv = p.Hkv, g = p.g;
-  const int RG = p.row_groups, KS = kGroupWaves / RG;   // row groups, waves that share a row group's keys
-  const int rg = wave & (RG - 1), kslot = RG == 1 ? wave : RG == 2 ? wave >> 1 : 0;
 
   // ---- lengths, and this workgroup's range of the list of all units' tiles.
   // Ranges are of equal cost: a tile costs 1 and a unit's start and end kUnitCost
@@ -204,7 +211,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
 
   // Ranges of cost / P, the first cost % P of them of one more
   const int cost = N + unit_cost * uniform(total_some) * Hkv;
-  const int P = min(p.P, N);
+  const int P = min(min(p.P, N), kMostPieces * uniform(total_some) * Hkv);
   if (pid >= P) return;
   const int share = uniform(cost / P), longer = cost - share * P;
   auto range_start = [&](int r) { return r * share + min(r, longer); };
@@ -232,7 +239,12 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
     int b, kvh, j0, j1, n, T, c;   // n: tiles of the unit
     int kend;                      // the first key past the segment
     int cost;                      // at which the unit begins
+    int groups;                    // (log2) groups of waves that have different rows of the unit
   };
+  // Of the four waves those of a row group share its keys, step by step in turn.
+  auto row_group = [&](const Segment& x) { return wave & ((1 << x.groups) - 1); };
+  auto key_slot = [&](const Segment& x) { return wave >> x.groups; };
+  auto stride = [&](const Segment& x) { return (kGroupWaves * kStep) >> x.groups; };   // keys from a wave's step to its next
   // (of the range: j1 = 0 if the unit is past its end)
   auto segment = [&](int b, int kvh, int j0, int at) {
     Segment x;
@@ -245,6 +257,10 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
     x.j1 = c_end >= at + x.n + unit_cost ? x.n : c_end > at ? cut_at(c_end - at, x.n) : 0;
     x.T = seq_T(s);
     x.c = seq_c(s);
+    // (as many as the unit's own rows need, whatever the longest chunk's do: 7 sequences
+    // of 22,000 keys, chunks of 3 to 15 with seven heads, float16: 114 us, so 105)
+    const int blocks = (x.c * g + kBlk * NRB - 1) / (kBlk * NRB);
+    x.groups = blocks <= 1 ? 0 : blocks <= 2 ? 1 : 2;
     x.kend = min(x.T, x.j1 * kTile);
     return x;
   };
@@ -297,7 +313,6 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
     int b, kvh, kend, base;
     int page[kStep / 8];
   };
-  const int by = kStep * KS;   // keys from a wave's step to its next
   auto aim = [&](Target& x, const Segment& at, int base) {
     x.b = at.b;
     x.kvh = at.kvh;
@@ -354,7 +369,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
     }
   };
 
-  // ---- queries: row block rb of the wave has the unit's rows 16 (NRB rg + rb) + lm.
+  // ---- queries: row block rb of a wave of row group rg has the unit's rows 16 (NRB rg + rb) + lm.
   // x / g for a row 0 <= x < 128 of a unit, by a float reciprocal: exact there, as
   // (x + 1/2) / g lies at least 1 / (2 g) from an integer
   const float inv_g = 1.f / (float)g;
@@ -365,6 +380,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
   // The entries of a lane: as of a key, the lg-th quarter of the row; with kCodes
   // 16 from 16 lg on, and from 64 + 16 lg on, as the MFMA takes its 8-bit operand.
   auto load_q = [&](const Segment& at) {
+    const int rg = row_group(at);
 #pragma unroll
     for (int rb = 0; rb < NRB; ++rb) {
       // (rows past the unit's are computed as its last one and not stored)
@@ -393,7 +409,7 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
   f32x4 o[NRB][DB];
   float m_run[NRB], m_use[NRB], l_lane[NRB];   // m_use: m_run, or 0 before any key
 
-  auto take_q = [&]() {
+  auto take_q = [&](int rg) {
 #pragma unroll
     for (int rb = 0; rb < NRB; ++rb) {
       tok[rb] = div_g(min(kBlk * (NRB * rg + rb) + lm, c * g - 1));
@@ -648,26 +664,28 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
   load_q(sg);
   {
     Target at;   // (both lookups before the first load)
-    aim(at, sg, sg.j0 * kTile + kStep * kslot);
-    aim(next, sg, sg.j0 * kTile + kStep * kslot + by);
+    const int base = sg.j0 * kTile + kStep * key_slot(sg);
+    aim(at, sg, base);
+    aim(next, sg, base + stride(sg));
     load(y, at);
   }
   for (;;) {
     const Segment nx = segment_after(sg);
     const bool more = nx.j1 > 0;
+    const int rg = row_group(sg), kslot = key_slot(sg), by = stride(sg), RG = 1 << sg.groups, KS = kGroupWaves >> sg.groups;
     l_ctx = sg.T - sg.c;
     c = sg.c;
-    take_q();
+    take_q(rg);
 
     // ---- this wave's steps of the segment.  follow(): the loads after those of
     // the step at base, and the lookup for the ones after them
-    const int first_base = kStep * kslot;   // of the next segment
+    const int first_base = kStep * key_slot(nx);
     auto follow = [&](Keys& z, int base) {
       const bool inside = base + by < sg.kend;
       if (!inside && more) aim(next, nx, first_base);   // (looked up late: once a segment)
       if (inside || more) load(z, next);
       if (base + 2 * by < sg.kend) aim(next, sg, base + 2 * by);
-      else if (!inside && more) aim(next, nx, first_base + by);
+      else if (!inside && more) aim(next, nx, first_base + stride(nx));
     };
     int base = sg.j0 * kTile + kStep * kslot;
     if (base >= sg.kend) follow(y, base);   // (none: the segment's last tile is short)
@@ -782,68 +800,79 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
   const bool m0 = uniform(sh_last[0]), m1 = n_pieces > 1 && uniform(sh_last[1]);
   const int n0 = m0 ? uniform(piece[0][3]) * (D / 4) : 0, n1 = m1 ? uniform(piece[1][3]) * (D / 4) : 0;
   const int pieces = max(m0 ? piece[0][1] - piece[0][0] : -1, m1 ? piece[1][1] - piece[1][0] : -1) + 1;   // of the larger
-  constexpr int kItems = 3, kBatch = 4;
-  for (int base = tid; base < n0 + n1; base += kItems * kGroupThreads) {
-    float m[kItems], z[kItems];
-    f32x4 acc[kItems];
-    int row[kItems], qf[kItems], ql[kItems], d[kItems], unit[kItems];
-#pragma unroll
-    for (int it = 0; it < kItems; ++it) {
-      const int idx = base + it * kGroupThreads;
-      const bool in0 = idx < n0;
-      const int local = in0 ? idx : idx - n0;
-      row[it] = local / (D / 4);
-      d[it] = 4 * (local - row[it] * (D / 4));
-      qf[it] = in0 ? piece[0][0] : piece[1][0];
-      ql[it] = idx < n0 + n1 ? (in0 ? piece[0][1] : piece[1][1]) : -1;   // (none for a thread past the items)
-      unit[it] = in0 ? piece[0][2] : piece[1][2];
-      m[it] = -INFINITY;
-      z[it] = 0.f;
-      acc[it] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    for (int k0 = 0; k0 < pieces; k0 += kBatch) {
-      float lse[kItems][kBatch];
-      f32x4 part[kItems][kBatch];
-#pragma unroll
-      for (int it = 0; it < kItems; ++it)
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-          lse[it][u] = -INFINITY;
-          part[it][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-          const int r = qf[it] + k0 + u;
-          if (r > ql[it]) continue;
-          const int at = (2 * r + (k0 + u == 0 ? 1 : 0)) * p.Rcap + row[it];
-          lse[it][u] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(ws_lse_rsrc, at * 4, 0, kDeviceCoherent));
-          part[it][u] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(ws_o_rsrc, (at * D + d[it]) * 4, 0,
-                                                                                        kDeviceCoherent));
-        }
+  auto merge = [&](auto items_at_once, auto pieces_at_once) {
+    constexpr int kItems = decltype(items_at_once)::value, kBatch = decltype(pieces_at_once)::value;
+    for (int base = tid; base < n0 + n1; base += kItems * kGroupThreads) {
+      float m[kItems], z[kItems];
+      f32x4 acc[kItems];
+      int row[kItems], qf[kItems], ql[kItems], d[kItems], unit[kItems];
 #pragma unroll
       for (int it = 0; it < kItems; ++it) {
-        float nm = m[it];
+        const int idx = base + it * kGroupThreads;
+        const bool in0 = idx < n0;
+        const int local = in0 ? idx : idx - n0;
+        row[it] = local / (D / 4);
+        d[it] = 4 * (local - row[it] * (D / 4));
+        qf[it] = in0 ? piece[0][0] : piece[1][0];
+        ql[it] = idx < n0 + n1 ? (in0 ? piece[0][1] : piece[1][1]) : -1;   // (none for a thread past the items)
+        unit[it] = in0 ? piece[0][2] : piece[1][2];
+        m[it] = -INFINITY;
+        z[it] = 0.f;
+        acc[it] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      for (int k0 = 0; k0 < pieces; k0 += kBatch) {
+        float lse[kItems][kBatch];
+        f32x4 part[kItems][kBatch];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) nm = fmaxf(nm, lse[it][u]);
-        const float nu = nm == -INFINITY ? 0.f : nm;
-        const float a = exp_diff(m[it], nu);
-        z[it] *= a;
-        acc[it] *= a;
-        m[it] = nm;
+        for (int it = 0; it < kItems; ++it)
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-          const float w = exp_diff(lse[it][u], nu);
-          z[it] += w;
-          acc[it] = add_weighted(acc[it], w, part[it][u]);
+          for (int u = 0; u < kBatch; ++u) {
+            lse[it][u] = -INFINITY;
+            part[it][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const int r = qf[it] + k0 + u;
+            if (r > ql[it]) continue;
+            const int at = (2 * r + (k0 + u == 0 ? 1 : 0)) * p.Rcap + row[it];
+            lse[it][u] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(ws_lse_rsrc, at * 4, 0, kDeviceCoherent));
+            part[it][u] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(ws_o_rsrc, (at * D + d[it]) * 4, 0,
+                                                                                          kDeviceCoherent));
+          }
+#pragma unroll
+        for (int it = 0; it < kItems; ++it) {
+          float nm = m[it];
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) nm = fmaxf(nm, lse[it][u]);
+          const float nu = nm == -INFINITY ? 0.f : nm;
+          const float a = exp_diff(m[it], nu);
+          z[it] *= a;
+          acc[it] *= a;
+          m[it] = nm;
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) {
+            const float w = exp_diff(lse[it][u], nu);
+            z[it] += w;
+            acc[it] = add_weighted(acc[it], w, part[it][u]);
+          }
         }
       }
-    }
 #pragma unroll
-    for (int it = 0; it < kItems; ++it) {
-      if (base + it * kGroupThreads >= n0 + n1) continue;
-      const int b = unit[it] / Hkv, kvh = unit[it] - b * Hkv, tk = div_g(row[it]);
-      const size_t orow = (size_t)(b * p.C_max + tk) * p.Hq + kvh * g + (row[it] - tk * g);
-      store_out<false, ELT>(p, orow * D + d[it], acc[it] * (z[it] > 0.f ? 1.f / z[it] : z[it] == 0.f ? 0.f : z[it]));
-      if (d[it] == 0) p.lse[orow] = z[it] == 0.f ? -INFINITY : m[it] + logf(z[it]);
+      for (int it = 0; it < kItems; ++it) {
+        if (base + it * kGroupThreads >= n0 + n1) continue;
+        const int b = unit[it] / Hkv, kvh = unit[it] - b * Hkv, tk = div_g(row[it]);
+        const size_t orow = (size_t)(b * p.C_max + tk) * p.Hq + kvh * g + (row[it] - tk * g);
+        store_out<false, ELT>(p, orow * D + d[it], acc[it] * (z[it] > 0.f ? 1.f / z[it] : z[it] == 0.f ? 0.f : z[it]));
+        if (d[it] == 0) p.lse[orow] = z[it] == 0.f ? -INFINITY : m[it] + logf(z[it]);
+      }
+    }
+  };
+  // Many pieces of few rows: more of a thread's loads are pieces (one sequence of 30000
+  // keys, 8 KV heads: 22.3 us, so 18.9).
+  if constexpr (NRB == 1) {
+    if (pieces > 8 && n0 + n1 <= 2 * kGroupThreads) {
+      merge(Int<1>{}, Int<16>{});
+      return;
     }
   }
+  merge(Int<3>{}, Int<4>{});
 }
 
 // ---------------------------------------------------------------- host side
@@ -882,7 +911,6 @@ void launch_kv4(const Kv4Params& p, hipStream_t stream) {
     // four heads: 47 us; one to a wave 18).
     const int blocks = (p.Rcap + kBlk - 1) / kBlk;
     const bool single = blocks == 1 || (ELT == kF32 && blocks <= 4);
-    s.row_groups = single ? (blocks <= 1 ? 1 : blocks <= 2 ? 2 : 4) : blocks <= 2 ? 1 : blocks <= 4 ? 2 : 4;
     if (single) hipLaunchKernelGGL((kv4_attn_kernel<ELT, D, PAGING, 1>), dim3(p.P), dim3(kGroupThreads), 0, stream, s);
     else hipLaunchKernelGGL((kv4_attn_kernel<ELT, D, PAGING, 2>), dim3(p.P), dim3(kGroupThreads), 0, stream, s);
   }

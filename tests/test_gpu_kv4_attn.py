@@ -192,6 +192,20 @@ def test_any_number_of_workgroups(grid):
     check(x, *call(x, grid_blocks=grid), label=f"grid {grid}")
 
 
+@pytest.mark.parametrize("grid", [1, 3, 17, 0])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_units_of_unlike_rows_in_one_range(grid, dtype):
+    """Chunks that need one, two and all four groups of waves, one after the other."""
+    x = make(22, dtype, [300, 9, 700, 1, 128, 260], [16, 1, 5, 12, 2, 9], Hq=16, Hkv=2, C=16, page=16)
+    check(x, *call(x, grid_blocks=grid), label=f"unlike rows {dtype} grid {grid}")
+
+
+@pytest.mark.parametrize("Hq,dtype", [(4, "bf16"), (12, "f16"), (12, "f32"), (40, "bf16")])
+def test_few_units_of_many_pieces(Hq, dtype):
+    x = make(23, dtype, [9000, 0, 6001], [1, 1, 2], Hq=Hq, Hkv=1, C=2, D=128)
+    check(x, *call(x), label=f"few units {Hq} {dtype}")
+
+
 def test_results_do_not_depend_on_timing():
     x = make(6, "f16", [3000, 700, 15], [5, 5, 5], page=16)
     first = call(x)
