@@ -21,8 +21,8 @@
 //
 // Measured (whole passes, 8 KV heads of 128, four query heads each): 32 sequences of
 // 16384 to 32768 in bfloat16, chunks of 4: 139 us, 6.3 TB/s, the stream's rate.  64 of 512
-// to 2048 in pages, chunks of 5: 34.7 us for 91 MB, of which start (lengths, lookups,
-// first loads) 4 to 5, a unit's end 2 and the pieces' join 4; 256 of them 95.  Trees of 16
+// to 2048 in pages, chunks of 5: 34 us for 92 MB, of which start (lengths, lookups,
+// first loads) 4 to 5, a unit's end 2 and the pieces' join 4; 256 of them 94.  Trees of 16
 // over the same contexts, float16: 69 us, bound by the vector instructions of its four
 // row blocks (60% of the issue slots, MFMA 25%).  4 sequences of 100 to 400, float32, D = 64,
 // single tokens: 9 us, a chain of launch, lengths, loads, join.
@@ -45,11 +45,15 @@ constexpr int kStep = 32;             // keys that a wave takes at a time: two M
 // The schedule (see the kernel): tiles a workgroup from which on units cost and cuts
 // snap, what a unit costs beside its tiles, and how near a unit's end a cut goes to it
 constexpr int kManyTiles = 6, kUnitCost = 4, kSnap = 3;
-// Pieces of a unit, about: its join is one workgroup's, a round trip for every few of
-// them (4 sequences of 23,000 keys, one KV head, chunks of 2, float16: 60 us with all
-// workgroups, 128 pieces; 33 with 32, 30 with 24; 3 sequences of 3,500 keys, 4 KV heads,
-// trees of 3 to 12: 46, 45, 53)
+// Pieces of a unit, at most and about: its join is one workgroup's, a round trip for
+// every few of them.  Up to one row block: 32 (4 sequences of 23,000 keys, one KV head,
+// chunks of 2, float16: 60 us with all workgroups, 128 pieces, and 33).  More rows, whose
+// join takes longer: a unit of n tiles in x pieces takes about a n / x + b x, least at a
+// multiple of sqrt(n), and twice that is near it (one sequence of 2,200 keys, 128 rows:
+// 18 pieces 39 us, 8 pieces 33; 13 of 3,700, one KV head, chunks of 3 to 14, float16: 70
+// and 65; 7 of 7,000, 4 KV heads, 126 rows, where 15 pieces leave a few CUs idle: 104, 111).
 constexpr int kMostPieces = 32;
+constexpr float kPiecesOfRoot = 2.f;
 
 template <int N>
 struct Int {
@@ -211,7 +215,10 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
 
   // Ranges of cost / P, the first cost % P of them of one more
   const int cost = N + unit_cost * uniform(total_some) * Hkv;
-  const int P = min(min(p.P, N), kMostPieces * uniform(total_some) * Hkv);
+  const int units = uniform(total_some) * Hkv;
+  const int most = NRB == 1 ? kMostPieces * min(units, p.P)
+                            : uniform((int)fminf(kPiecesOfRoot * sqrtf((float)N * (float)units), (float)p.P));
+  const int P = min(min(p.P, N), most);
   if (pid >= P) return;
   const int share = uniform(cost / P), longer = cost - share * P;
   auto range_start = [&](int r) { return r * share + min(r, longer); };
@@ -872,7 +879,8 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
       return;
     }
   }
-  merge(Int<3>{}, Int<4>{});
+  if (NRB > 1 && pieces > 4) merge(Int<3>{}, Int<8>{});   // (32 pieces of 126 rows, 7 sequences: 114 us, so 104)
+  else merge(Int<3>{}, Int<4>{});
 }
 
 // ---------------------------------------------------------------- host side
