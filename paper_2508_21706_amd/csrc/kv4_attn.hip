@@ -20,7 +20,7 @@
 // by the last one to arrive.
 //
 // Measured (whole passes, 8 KV heads of 128, four query heads each): 32 sequences of
-// 16384 to 32768 in bfloat16, chunks of 4: 139 us, 6.3 TB/s, the stream's rate.  64 of 512
+// 16384 to 32768 in bfloat16, chunks of 4: 141 us, 6.2 TB/s, near the stream's rate.  64 of 512
 // to 2048 in pages, chunks of 5: 34 us for 92 MB, of which start (lengths, lookups,
 // first loads) 4 to 5, a unit's end 2 and the pieces' join 4; 256 of them 94.  Trees of 16
 // over the same contexts, float16: 69 us, bound by the vector instructions of its four
