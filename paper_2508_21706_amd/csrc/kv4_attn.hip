@@ -97,13 +97,15 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// The largest of 8 scores, NaN aside
+// The largest of 8 scores, NaN if one is: three instructions of three operands and one
+// of two, without the canonicalising that fmaxf adds for each of an MFMA's results.
+// (Not by inline assembly, as the wait that an MFMA's results need before a vector
+// instruction reads them is the compiler's, and it does not look into assembly.)
 __device__ __forceinline__ float max8(const float (&y)[8]) {
-  float a, b;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(y[0]), "v"(y[1]), "v"(y[2]));
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(b) : "v"(y[3]), "v"(y[4]), "v"(y[5]));
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(a), "v"(y[6]), "v"(y[7]));
-  return fmaxf(a, b);
+  float a = y[0];
+#pragma unroll
+  for (int e = 1; e < 8; ++e) a = __builtin_elementwise_maximum(a, y[e]);
+  return a;
 }
 
 // Two values cut to their leading 8 significant bits, as two bfloat16; x keeps
