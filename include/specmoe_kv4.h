@@ -88,7 +88,12 @@ int specmoe_append_kv4(const void* q, const void* k, const void* v, const void* 
  * probabilities are rounded to bfloat16 when dtype is bfloat16, and kept to 16
  * bits for float16 and 24 for float32.  Padding rows and tokens that see no key
  * get out = 0 and lse = -inf.  Keys that a token does not see leave its results
- * alone whatever they hold, NaN blocks included.
+ * alone whatever they hold, NaN blocks and values past float32's range included.
+ * Such values are infinities to the tokens that see them: their entries of the
+ * result are infinities or NaN.  (Sums over the values are divided by the
+ * probabilities' sum at the end and taken with weights up to 2^8 until then: over
+ * 2^24 keys values from 2^96 on can pass float32's range on the way, and become
+ * infinities too.)
  *
  * The workspace is one of specmoe_verify_attn (same zeroed region, initialised
  * by specmoe_verify_attn_workspace_init) of at least

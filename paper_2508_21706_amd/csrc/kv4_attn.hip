@@ -120,6 +120,9 @@ __device__ __forceinline__ uint32_t split2(float& x, float& y) {
   return (p >> 16) | q;
 }
 
+// The least scale byte whose unit, 2^126, has a code (4 units) past float32's range
+constexpr uint32_t kFarByte = 253;
+
 // (kCodes) 16 values as 8-bit codes of `unit`, to nearest even; x keeps what the
 // rounding left.  An infinity or NaN has the NaN code.
 __device__ __forceinline__ void part8(float (&x)[16], float unit, bool rest, int* codes) {
@@ -479,20 +482,21 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
 
   auto compute = [&](Keys& x, int base) {
     const bool drafts = base + kStep > l_ctx;   // (the same for the whole wave) keys that not every row sees
-    // NaN blocks among the values of such keys: 0 times NaN would reach the rows
-    // that do not see them, so they are staged as zeros, and the rows that see them
-    // made NaN afterwards.  Bit 16 qd + i of nan[h]: the qd-th quarter of key 16 h + i.
-    uint64_t nan[2] = {0, 0};
+    // Values of such keys that are infinities or NaN (scale bytes from kFarByte on can
+    // make them): 0 times them would reach the rows that do not see the key.  So these
+    // blocks are staged with scale byte 0, too small to show, and added to the rows that
+    // see them afterwards; their bytes lie behind their rows in the stage.  Bit 16 qd + i
+    // of far[h]: the qd-th quarter of key 16 h + i.
+    uint64_t far[2] = {0, 0};
     uint32_t seen[NRB];   // (drafts) bit e: the lane's row sees its e-th key
     if (drafts) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const bool bad = x.vs[h] == 255u;
-        nan[h] = __ballot(bad);
-        if (bad) {
+        const bool is_far = x.vs[h] >= kFarByte;
+        far[h] = __ballot(is_far);
+        if (is_far) {
+          *reinterpret_cast<uint32_t*>(stage + (kBlk * h + lm) * kPitch + 2 * D + 4 * lg) = x.vs[h];
           x.vs[h] = 0;
-#pragma unroll
-          for (int w = 0; w < KW; ++w) x.v[h][w] = 0;
         }
       }
     }
@@ -639,19 +643,42 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
     }
     __builtin_amdgcn_sched_group_barrier(kMfma, NRB * PP * kAheadV, 0);
     asm volatile("" ::: "memory");
-    if (nan[0] | nan[1]) {
+    if (far[0] | far[1]) {
+      // one key after the other, as the MFMA takes it: the probability's parts times the
+      // value, for the rows that see the key
 #pragma unroll
-      for (int rb = 0; rb < NRB; ++rb) {
-        const uint32_t own0 = (seen[rb] & 15u) << (4 * lg), own1 = (seen[rb] >> 4) << (4 * lg);
-        uint32_t hit = 0;   // bit qd: the row sees a NaN block in the qd-th quarter
+      for (int h = 0; h < 2; ++h) {
+        uint32_t keys = (uint32_t)(far[h] | far[h] >> 16 | far[h] >> 32 | far[h] >> 48) & 0xffffu;
+        for (; keys; keys &= keys - 1) {
+          const int i = __builtin_ctz(keys);
+          const char* row = stage + (kBlk * h + i) * kPitch;
+          const int src = lm + kBlk * (i >> 2);   // the lane that has the key's probability
 #pragma unroll
-        for (int qd = 0; qd < 4; ++qd)
-          if (((uint32_t)(nan[0] >> (16 * qd)) & own0) | ((uint32_t)(nan[1] >> (16 * qd)) & own1)) hit |= 1u << qd;
-        hit |= (uint32_t)__shfl_xor((int)hit, 16);
-        hit |= (uint32_t)__shfl_xor((int)hit, 32);
+          for (int rb = 0; rb < NRB; ++rb) {
+            const bool sees = (uint32_t)__shfl((int)seen[rb], src) >> (4 * h + (i & 3)) & 1u;
+            float pr = 0.f;
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
-          if ((hit >> (db / (DB / 4))) & 1u) o[rb][db] = f32x4{NAN, NAN, NAN, NAN};
+            for (int part = PP - 1; part >= 0; --part) {
+              const uint32_t pair = (i & 2) ? pb[rb][part][2 * h + 1] : pb[rb][part][2 * h];
+              const uint32_t both = (uint32_t)__shfl((int)pair, src);
+              pr += __uint_as_float((i & 1) ? both & 0xffff0000u : both << 16);
+            }
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+              constexpr int kPerQuarter = DB / 4;
+              if (!((far[h] >> (16 * (db / kPerQuarter) + i)) & 1u)) continue;
+              const uint32_t byte = *reinterpret_cast<const uint32_t*>(row + 2 * D + 4 * (db / kPerQuarter));
+              const uint2 v = *reinterpret_cast<const uint2*>(row + 32 * db + 8 * lg);
+              const float unit = byte == 255u ? NAN : kv4::scale_of(byte);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const uint32_t w = r < 2 ? v.x : v.y;
+                const float code = __uint_as_float((r & 1) ? w & 0xffff0000u : w << 16) * 0x1p127f;
+                if (sees) o[rb][db][r] = fmaf(pr, code * unit, o[rb][db][r]);
+              }
+            }
+          }
+        }
       }
     }
   };

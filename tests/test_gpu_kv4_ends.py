@@ -1,0 +1,135 @@
+"""verify_attn_kv4 where the cache holds values past float32's range: scale bytes 253 and
+254, whose codes of 4 and more (2 and more) units are infinities as float32, and 255.
+
+A token that does not see such a key has the bits that it has without it.  One that
+sees it has, in the block, the infinities of its entries with their signs, and of the
+finite ones (a few 2^126, beside which the other keys vanish) p v or, where the sum passes
+float32's range on the way, their infinity, wherever the key lies:
+in a step of the context alone, in one with drafts, among the drafts.  (Where float16's
+and float32's probabilities are several bfloat16 parts, of unlike signs or 0, a step of the
+context alone makes NaN of an infinity.)"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2508_21706_amd as pkg
+from oracle.kv4 import decode_ref, encode_ref
+from oracle.step import scored_row_ref
+from test_gpu_append import f64
+from test_gpu_kv4_attn import HP, TYPES, call, make, on_gpu, sees_of
+from test_gpu_parity import dev, note
+
+pytestmark = pytest.mark.gpu
+
+CTX, CHUNK = [45, 3], [6, 6]
+EVERY_CODE = np.array([0x10, 0x32, 0x54, 0x76, 0x98, 0xba, 0xdc, 0xfe] * 2, np.uint8)   # each code twice
+
+
+def put(x, key, byte, head=0, block=1):
+    """Values of one key of sequence 0: every code, in units of the byte's."""
+    x["slab"][2][0, head, key, 16 * block:16 * block + 16] = EVERY_CODE
+    x["slab"][3][0, head, key, block] = byte
+
+
+def check_far(x, key, byte, label):
+    dtype, D, g = x["dtype"], x["D"], x["q"].shape[2] // x["slab"][0].shape[1]
+    clean = [t.copy() for t in x["slab"]]
+    put(x, key, byte)
+    cache, table = on_gpu(x)
+    out, lse = call(x, cache, table)
+    again = call(x, cache, table)
+    assert all(torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0)) for a, b in zip((out, lse), again)), label
+    dirty, x["slab"] = x["slab"], clean
+    clean[2][0, 0, key, 16:32], clean[3][0, 0, key, 1] = 0, 1     # (nothing from this key's block)
+    ref, ref_lse = call(x)
+    x["slab"] = dirty
+    assert torch.equal(lse, ref_lse), f"{label}: lse"
+    v = decode_ref(EVERY_CODE[None], np.array([[byte]], np.uint8))[0]
+    with np.errstate(over="ignore"):
+        as_f32 = v.astype(np.float32).astype(np.float64)
+    k = decode_ref(x["slab"][0][0, 0, :51], x["slab"][1][0, 0, :51])
+    h, most = torch.finfo(TYPES[dtype]).eps / 2, torch.finfo(TYPES[dtype]).max
+    seen_by = 0
+    for b in range(2):
+        for i in range(CHUNK[b]):
+            sees = sees_of(x, b, i)
+            for head in range(x["q"].shape[2]):
+                o, r = out[b, i, head], ref[b, i, head]
+                if b or head >= g or not sees[key]:
+                    assert torch.equal(o, r), f"{label}: {b} {i} {head} does not see the key"
+                    continue
+                seen_by += 1
+                assert torch.equal(o[:32], r[:32]) and torch.equal(o[64:], r[64:]), f"{label}: other blocks of {i} {head}"
+                got = f64(o[32:64])
+                _, s = scored_row_ref(f64(x["q"])[b, i, head], k, k, x["scale"], sees)
+                p = np.exp(float(k[key] @ f64(x["q"])[b, i, head]) * x["scale"] - s)
+                for e in range(32):
+                    if byte == 255:
+                        assert np.isnan(got[e]), f"{label}: {i} {head} {e}"
+                    elif v[e] == 0:
+                        assert got[e] == f64(r)[32 + e], f"{label}: {i} {head} {e}"
+                    elif np.isinf(as_f32[e]) or p * abs(v[e]) > 2 * most:
+                        parts = dtype != "bf16" and key < 32
+                        assert got[e] == np.copysign(np.inf, v[e]) or parts and np.isnan(got[e]), f"{label}: {i} {head} {e}"
+                    else:
+                        # Weights are relative to a maximum that a score may pass by 8 binades before
+                        # it moves, and divided by their sum at the end: w v is up to 2^8 2^125 = 2^133
+                        # for the least of these entries, 1/2 2^126, and float32 ends at 2^128, so any
+                        # of them may pass it on the way.
+                        if got[e] == np.copysign(np.inf, v[e]):
+                            continue
+                        # (2^-12: scores and statistics of a few dozen keys, far more than they are off)
+                        want = p * v[e]
+                        assert abs(got[e] - want) <= (HP[dtype] + h + 2.0 ** -12) * abs(want) * (1 + h), f"{label}: {i} {head} {e}"
+    assert seen_by
+    note(f"[kv4 {label}] seen by {seen_by} rows")
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(2, 2), (12, 1)])
+@pytest.mark.parametrize("dtype,D,page", [("bf16", 128, 0), ("bf16", 128, 8), ("bf16", 64, 16), ("f16", 128, 16),
+                                          ("f16", 64, 8), ("f32", 128, 8), ("f32", 64, 0)])
+@pytest.mark.parametrize("tree", [False, True])
+def test_values_past_float32(dtype, D, page, tree, Hq, Hkv):
+    """One and two row blocks to a wave."""
+    x = make(80, dtype, CTX, CHUNK, Hq=Hq, Hkv=Hkv, D=D, C=6, page=page, tree=tree)
+    if tree:   # 0 - 1 - 2, 0 - 3 - 4, 5 alone
+        x["words"][:] = np.array([1, 3, 7, 9, 25, 32], np.uint64)
+    for key in (10, 40, 45 + 3):
+        for byte in (253, 254, 255):
+            one = dict(x, slab=[t.copy() for t in x["slab"]])
+            check_far(one, key, byte, f"{dtype} {D} page {page} tree {tree} {Hq}/{Hkv} key {key} byte {byte}")
+
+
+def test_tokens_that_see_nothing_stay_zero():
+    x = make(81, "bf16", [0], [4], Hq=4, Hkv=1, C=4, tree=True)
+    x["words"][:] = np.array([0, 2, 6, 8], np.uint64)
+    for block in range(4):
+        put(x, 0, 253 + block % 2, block=block)
+    out, lse = call(x)
+    x["slab"][3][0, 0, 0] = 1
+    ref, ref_lse = call(x)
+    assert (out[0, 0] == 0).all() and (lse[0, 0] == -np.inf).all()
+    assert torch.equal(out, ref) and torch.equal(lse, ref_lse)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_finite_entries_appended(dtype):
+    """Entries from 1.75 2^127 on go to 4 units of 2^126, 2^128: an infinity of float32 for
+    the draft itself and the ones after it, nothing for those before."""
+    x = make(82, dtype, [20], [4], Hq=2, Hkv=1, C=4)
+    d = dev()
+    cache, _ = on_gpu(x)
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=d)   # noqa: E731
+    k = torch.randn((1, 4, 1, 128), generator=torch.Generator().manual_seed(82)).to(TYPES[dtype])
+    v = k.clone()
+    v[0, 2, 0, 7], v[0, 2, 0, 8] = torch.finfo(TYPES[dtype]).max, -1.5 * 2.0 ** 127
+    for values in (v, k):
+        pkg.append_kv4(None, k.to(d), values.to(d), cache, i32([20]), i32([4]))
+        if values is v:
+            assert np.array_equal(cache.v_scales[0, 0, 22].cpu().numpy(), encode_ref(f64(v[0, 2, 0]))[1])
+            assert int(cache.v_scales[0, 0, 22, 0]) == 253
+            out, lse = call(x, cache)
+    ref, ref_lse = call(x, cache)
+    assert torch.equal(lse, ref_lse) and torch.equal(out[0, :2], ref[0, :2])
+    assert (out[0, 2:, :, 7] == np.inf).all() and (out[0, 2:, :, 8] < -2.0 ** 100).all()
+    assert torch.equal(out[0, 2:, :, 32:], ref[0, 2:, :, 32:])
