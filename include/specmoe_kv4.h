@@ -83,11 +83,13 @@ int specmoe_append_kv4(const void* q, const void* k, const void* v, const void* 
  * statistics of the softmax.  Queries are taken exactly, but for entries under
  * 2^-13 of the largest of their block of 32 in a 16-bit type with D = 128: such
  * an entry is off by at most 2^-22 (bfloat16) or 2^-27 (float16) of that largest
- * one.  A query that holds an infinity or NaN, or
- * whose product with a key it sees passes float32's range, gets NaN.  For their product with the values,
- * probabilities are rounded to bfloat16 when dtype is bfloat16, and kept to 16
- * bits for float16 and 24 for float32.  Padding rows and tokens that see no key
- * get out = 0 and lse = -inf.  Keys that a token does not see leave its results
+ * one.  A query that holds an infinity or NaN gets NaN, and so does one whose
+ * score with a key it sees passes float32's range upwards, or downwards with every
+ * key that it sees; a key whose score alone passes it downwards (-inf) has no
+ * weight.  For their product with the values, probabilities are rounded to
+ * bfloat16 when dtype is bfloat16, and kept to 16 bits for float16 and 24 for
+ * float32.  Padding rows and tokens that see no key get out = 0 and lse = -inf.
+ * Keys that a token does not see leave its results
  * alone whatever they hold, NaN blocks and values past float32's range included.
  * Such values are infinities to the tokens that see them: their entries of the
  * result are infinities or NaN.  (Sums over the values are divided by the

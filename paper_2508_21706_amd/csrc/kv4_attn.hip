@@ -683,6 +683,13 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
     }
   };
 
+  // A token of n in its chunk that sees a key: one of the l of its context, or one that
+  // its word names (in a chain always itself).  If no key that such a token sees has any
+  // weight, all of their scores are -inf and the row is NaN, not empty.
+  auto sees_any = [&](uint64_t w, int l, int n) {
+    return l > 0 || !p.draft_mask || (w & (n >= 64 ? ~0ull : (1ull << n) - 1)) != 0;
+  };
+
   // pieces of units that other workgroups share, at most the range's first and
   // last: the first and last range that have a piece of the unit, its index, its rows
   int n_pieces = 0;
@@ -774,12 +781,13 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
         wk[k] = __builtin_amdgcn_exp2f(mk[k] - Mu);
         L += (k & (RG - 1)) == rg ? lk[k] * wk[k] : 0.f;
       }
-      const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;   // (a NaN stays)
+      const bool lost = L == 0.f && whole && sees_any(word[rb], l_ctx, c);
+      const float inv = L > 0.f ? 1.f / L : lost ? NAN : L == 0.f ? 0.f : L;   // (a NaN stays)
       const int row = kBlk * (NRB * rg + rb) + lm;
       const bool valid = row < R;
       const size_t orow = (size_t)(sg.b * p.C_max + tok[rb]) * p.Hq + sg.kvh * g + (row - tok[rb] * g);
       if (valid && kslot == 0 && lg == 0) {
-        const float lse = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+        const float lse = lost ? NAN : L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
         if (whole) p.lse[orow] = lse;
         else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(int, lse), ws_lse_rsrc, (slot * p.Rcap + row) * 4, 0,
                                                    kDeviceCoherent);
@@ -895,8 +903,14 @@ __global__ __launch_bounds__(kGroupThreads, 2) void kv4_attn_kernel(Kv4Params p)
         if (base + it * kGroupThreads >= n0 + n1) continue;
         const int b = unit[it] / Hkv, kvh = unit[it] - b * Hkv, tk = div_g(row[it]);
         const size_t orow = (size_t)(b * p.C_max + tk) * p.Hq + kvh * g + (row[it] - tk * g);
-        store_out<false, ELT>(p, orow * D + d[it], acc[it] * (z[it] > 0.f ? 1.f / z[it] : z[it] == 0.f ? 0.f : z[it]));
-        if (d[it] == 0) p.lse[orow] = z[it] == 0.f ? -INFINITY : m[it] + logf(z[it]);
+        bool lost = z[it] == 0.f;
+        if (lost) {
+          const uint32_t s = seqs[b];
+          lost = sees_any(p.draft_mask ? p.draft_mask[b * p.C_max + tk] : 0ull, seq_T(s) - seq_c(s), seq_c(s));
+        }
+        store_out<false, ELT>(p, orow * D + d[it],
+                              acc[it] * (z[it] > 0.f ? 1.f / z[it] : lost ? NAN : z[it] == 0.f ? 0.f : z[it]));
+        if (d[it] == 0) p.lse[orow] = lost ? NAN : z[it] == 0.f ? -INFINITY : m[it] + logf(z[it]);
       }
     }
   };

@@ -133,3 +133,66 @@ def test_large_finite_entries_appended(dtype):
     assert torch.equal(lse, ref_lse) and torch.equal(out[0, :2], ref[0, :2])
     assert (out[0, 2:, :, 7] == np.inf).all() and (out[0, 2:, :, 8] < -2.0 ** 100).all()
     assert torch.equal(out[0, 2:, :, 32:], ref[0, 2:, :, 32:])
+
+
+TYPES_DIMS = [("bf16", 64), ("bf16", 128), ("f16", 64), ("f16", 128), ("f32", 64), ("f32", 128)]
+
+
+def opposed(seed, dtype, D, ctx, chunk, entry=5, **kw):
+    """Queries of one sign at an entry where every key has the other: a score of -inf with
+    each key if the entry is infinite."""
+    x = make(seed, dtype, ctx, chunk, Hq=4, Hkv=1, D=D, **kw)
+    assert entry % 2
+    x["slab"][0][..., entry // 2] = x["slab"][0][..., entry // 2] & 0x0F | 0xC0   # code 12: -2
+    x["q"][..., entry] = x["q"][..., entry].abs()
+    return x
+
+
+@pytest.mark.parametrize("dtype,D", TYPES_DIMS)
+@pytest.mark.parametrize("grid", [0, 1, 3])
+def test_an_infinite_entry_against_keys_of_the_other_sign(dtype, D, grid):
+    """NaN, not the row of a token that sees nothing; in whole units and cut ones."""
+    x = opposed(83, dtype, D, [0, 50, 700], [2, 3, 1], C=3)
+    ref, ref_lse = call(x, grid_blocks=grid)
+    hit = torch.zeros(ref_lse.shape, dtype=torch.bool, device=dev())
+    for b, i, h in ((0, 0, 0), (0, 1, 3), (1, 2, 1), (2, 0, 0), (2, 0, 2)):
+        x["q"][b, i, h, 5] = float("inf")
+        hit[b, i, h] = True
+    out, lse = call(x, grid_blocks=grid)
+    assert torch.isnan(out[hit]).all() and torch.isnan(lse[hit]).all()
+    assert torch.equal(out[~hit], ref[~hit]) and torch.equal(lse[~hit], ref_lse[~hit])
+
+
+@pytest.mark.parametrize("dtype,D", TYPES_DIMS)
+@pytest.mark.parametrize("grid", [0, 2])
+def test_infinite_entries_of_trees(dtype, D, grid):
+    """Tokens that see a draft or the context get NaN, those that see nothing stay empty."""
+    x = opposed(84, dtype, D, [0, 260], [4, 4], C=4, tree=True)
+    x["words"][:] = np.array([[0, 2, 16, 9], [0, 2, 6, 1 << 63]], np.uint64)   # (bits past the chunk are ignored)
+    x["q"][:, :4, :, 5] = float("inf")
+    out, lse = call(x, grid_blocks=grid)
+    empty = [(0, 0), (0, 2)]
+    for b in range(2):
+        for i in range(4):
+            if (b, i) in empty:
+                assert (out[b, i] == 0).all() and (lse[b, i] == -np.inf).all(), (b, i)
+            else:
+                assert torch.isnan(out[b, i]).all() and torch.isnan(lse[b, i]).all(), (b, i)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+def test_scores_past_float32(dtype, D):
+    """-2 2^127 -2 2^127 = -2^129 with every key: NaN.  Where one key has codes 0 at both
+    entries, that key alone has weight."""
+    x = opposed(85, dtype, D, [40, 9], [1, 1], C=1)
+    for entry in (4, 6):   # (low halves of their bytes)
+        x["slab"][0][..., entry // 2] = x["slab"][0][..., entry // 2] & 0xF0 | 0x0C
+    x["slab"][1][..., 0] = np.where(x["slab"][1][..., 0] == 255, 255, 127)
+    q = torch.zeros_like(x["q"])
+    q[..., 4], q[..., 6] = 2.0 ** 127, 2.0 ** 127
+    x["q"] = q
+    x["slab"][0][1, 0, 3] = 0
+    out, lse = call(x)
+    assert torch.isnan(out[0]).all() and torch.isnan(lse[0]).all()
+    v = decode_ref(x["slab"][2][1, 0, 3], x["slab"][3][1, 0, 3])
+    assert (f64(out[1, 0]) == v).all() and (lse[1, 0] == 0).all()
