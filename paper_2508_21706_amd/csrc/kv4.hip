@@ -318,7 +318,7 @@ __global__ __launch_bounds__(kReadThreads) void read_kv4_kernel(ReadParams p) {
   constexpr int kElt = ELT == kF32 ? 4 : 2;
   constexpr int LK = D / 8;
   const int b = blockIdx.x / p.tiles, i0 = (blockIdx.x - b * p.tiles) * kReadTokens;
-  const int n = min(p.rows[b], p.N_max) - i0;
+  const int n = min(max(p.rows[b], 0), p.N_max) - i0;
   if (n <= 0) return;
   const int64_t first = (int64_t)max(p.first[b], 0) + i0;
   const char* codes = blockIdx.y == 0 ? p.cache.k_codes : p.cache.v_codes;
