@@ -86,12 +86,13 @@ __device__ int block_scan(int x, int* sums, int* waves, int& total) {
 //
 // A search is ten dependent LDS reads and the page a load behind them; kTogether of both
 // are in flight (17,000 pages: 21.7 us a step with its slots, one at a time 24.8).
+// (Indexes past the last page, which may be the 2^31st, stay below 2^32.)
 template <int kTogether, class Place>
 __device__ __forceinline__ void copy_list(const int* sums, int n, const Place& place) {
-  for (int i0 = threadIdx.x; i0 < n; i0 += kTogether * kThreads) {
+  for (uint32_t i0 = threadIdx.x; i0 < (uint32_t)n; i0 += kTogether * kThreads) {
     int at[kTogether], lo[kTogether];
 #pragma unroll
-    for (int u = 0; u < kTogether; ++u) at[u] = min(i0 + u * kThreads, n - 1), lo[u] = 0;
+    for (int u = 0; u < kTogether; ++u) at[u] = (int)min(i0 + u * kThreads, (uint32_t)n - 1), lo[u] = 0;
     // the first thread whose inclusive sum exceeds the item's index
 #pragma unroll
     for (int step = kThreads / 2; step; step >>= 1)

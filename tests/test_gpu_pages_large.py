@@ -1,0 +1,36 @@
+"""assign_pages at the ends of its sizes: lists of pages near 2^31."""
+import pytest
+import torch
+
+import paper_2508_21706_amd as pkg
+from test_gpu_pages import i32
+from test_gpu_parity import dev, note
+
+pytestmark = pytest.mark.gpu
+
+PART = 1 << 28
+
+
+def equal(a, b):
+    """Of flat tensors, a part at a time."""
+    return len(a) == len(b) and all(torch.equal(a[i:i + PART], b[i:i + PART]) for i in range(0, len(a), PART))
+
+
+def test_almost_2_to_31_pages_returned_and_taken():
+    B, per = 8, (1 << 28) - 1
+    n = B * per
+    note(f"case {n} pages")
+    before = torch.arange(n, dtype=torch.int32, device=dev())
+    state = pkg.PageState(before.clone().view(B, per), i32([per] * B),
+                          torch.full(((1 << 31) - 1,), -3, dtype=torch.int32, device=dev()), i32([0]))
+    pkg.assign_pages(i32([0] * B), i32([0] * B), state, 8, max_chunk=1)
+    torch.cuda.synchronize()
+    assert int(state.free_count) == n and (state.held == 0).all()
+    assert equal(state.free_pages[:n], before) and (state.free_pages[n:] == -3).all()
+    missing, _ = pkg.assign_pages(i32([8 * per] * B), i32([0] * B), state, 8, max_chunk=1)
+    torch.cuda.synchronize()
+    assert int(state.free_count) == 0 and (state.held == per).all() and not missing.any()
+    table = state.block_table.view(-1)
+    for i in range(0, n, PART):   # the top page first
+        part = table[i:i + PART]
+        assert torch.equal(part, torch.arange(n - 1 - i, n - 1 - i - len(part), -1, dtype=torch.int32, device=dev()))
