@@ -118,8 +118,9 @@ __device__ __forceinline__ void copy_pages(const int* sums, int n, const Place& 
 }
 
 __device__ __forceinline__ int64_t slot_of(const Params& p, int b, const Need& n, int held, int i) {
-  const int pos = n.l + i;
-  if (i >= n.c || (pos >> p.page_shift) >= held) return -1;
+  if (i >= n.c) return -1;
+  const int pos = n.l + i;   // (< 2^31, as l + c is)
+  if ((pos >> p.page_shift) >= held) return -1;
   const int64_t page = p.table[(size_t)b * p.pages_per_seq + (pos >> p.page_shift)];
   return (page << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
 }
@@ -253,7 +254,7 @@ extern "C" int specmoe_assign_pages(const int32_t* ctx_lens, const int32_t* chun
   (void)hipGetLastError();
   hipLaunchKernelGGL(assign_kernel, dim3(1), dim3(kThreads), 0, s, p, own ? 1 : 0);
   if (slots && !own)
-    hipLaunchKernelGGL(slots_kernel, dim3((desc->C_max + kSlotThreads - 1) / kSlotThreads, desc->B), dim3(kSlotThreads),
-                       0, s, p);
+    hipLaunchKernelGGL(slots_kernel, dim3((unsigned)(((int64_t)desc->C_max + kSlotThreads - 1) / kSlotThreads), desc->B),
+                       dim3(kSlotThreads), 0, s, p);
   return hipGetLastError() == hipSuccess ? SPECMOE_OK : SPECMOE_ERR_LAUNCH;
 }

@@ -1,4 +1,4 @@
-"""assign_pages at the ends of its sizes: lists of pages near 2^31."""
+"""assign_pages at the ends of its sizes: lists of pages and slot maps near 2^31."""
 import pytest
 import torch
 
@@ -34,3 +34,21 @@ def test_almost_2_to_31_pages_returned_and_taken():
     for i in range(0, n, PART):   # the top page first
         part = table[i:i + PART]
         assert torch.equal(part, torch.arange(n - 1 - i, n - 1 - i - len(part), -1, dtype=torch.int32, device=dev()))
+
+
+@pytest.mark.parametrize("short", [1, 100, 300])
+def test_a_slot_map_of_almost_2_to_31(short):
+    """One request's chunk: as many tokens as its pages hold, -1 behind them."""
+    page, C = 65536, (1 << 31) - short
+    per = (1 << 31) // page - 1
+    note(f"case {C} slots")
+    state = pkg.alloc_page_state(1, per, per, dev())
+    slots = torch.full((1, C), -7, dtype=torch.int64, device=dev())
+    missing, _ = pkg.assign_pages(i32([3]), i32([(1 << 31) - 1]), state, page, slots=slots)
+    torch.cuda.synchronize()
+    assert int(state.free_count) == 0 and int(state.held) == per and not missing.any()
+    c = page * per - 3
+    for i in range(0, c, PART):   # (page k is the k-th to be taken)
+        part = slots[0, i:min(i + PART, c)]
+        assert torch.equal(part, torch.arange(i + 3, i + 3 + len(part), device=dev()))
+    assert (slots[0, c:] == -1).all()
