@@ -74,8 +74,9 @@ int specmoe_append_kv4(const void* q, const void* k, const void* v, const void* 
  *                i >= c_b are never read.
  *   cache        host pointer to the cache.  Rows >= l_b + c_b are never read.
  *   out          device, 16-byte aligned: [B, C_max, Hq, D] of dtype (the type
- *                that the projection after it takes); not q's memory.
- *   lse          device, float32 [B, C_max, Hq].
+ *                that the projection after it takes).
+ *   lse          device, float32 [B, C_max, Hq].  q, out and lse share no
+ *                memory (SPECMOE_ERR_OVERLAP, after all other checks).
  *   desc         as in specmoe_verify_attn; dtype is the type of q and out.
  *                grid_blocks 0: 512 workgroups, two per CU.
  *

@@ -75,9 +75,11 @@ enum {
   SPECMOE_ERR_ROPE = -16,         /* (specmoe_append_kv) rot_dim is not a multiple of 16
                                      in [0, D], rope_style is not a specmoe_rope_style,
                                      or norm_eps is negative or not finite           */
-  SPECMOE_ERR_SCORE = -17         /* (specmoe_verify_attn_scored) softcap or window is
+  SPECMOE_ERR_SCORE = -17,        /* (specmoe_verify_attn_scored) softcap or window is
                                      negative, or softcap or scale / softcap is not
                                      finite                                          */
+  SPECMOE_ERR_OVERLAP = -18       /* (specmoe_verify_attn_kv4) out, lse and q share
+                                     memory                                          */
 };
 
 /* desc->flags bits. */

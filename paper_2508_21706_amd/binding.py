@@ -25,7 +25,7 @@ STATUS = {
     -4: "SPECMOE_ERR_HEAD_DIM", -5: "SPECMOE_ERR_DTYPE", -6: "SPECMOE_ERR_ROWS", -7: "SPECMOE_ERR_GRID",
     -8: "SPECMOE_ERR_WORKSPACE", -9: "SPECMOE_ERR_ALIGN", -10: "SPECMOE_ERR_SCALE", -11: "SPECMOE_ERR_LAUNCH",
     -12: "SPECMOE_ERR_FLAGS", -13: "SPECMOE_ERR_MASK", -14: "SPECMOE_ERR_PAGES", -15: "SPECMOE_ERR_HANDOFF",
-    -16: "SPECMOE_ERR_ROPE", -17: "SPECMOE_ERR_SCORE",
+    -16: "SPECMOE_ERR_ROPE", -17: "SPECMOE_ERR_SCORE", -18: "SPECMOE_ERR_OVERLAP",
 }
 ROPE_STYLES = {"halves": 0, "pairs": 1}   # specmoe_rope_style
 SPECMOE_FLAG_NO_WAIT = 1
@@ -1049,7 +1049,7 @@ def verify_attn_kv4(q: torch.Tensor, cache: KV4Cache, ctx_lens: torch.Tensor, ch
         lse = _empty((B, C_max, Hq), torch.float32, q.device, stream)
     _check_on(out, "out", (B, C_max, Hq, D), dt, dev)
     _check_on(lse, "lse", (B, C_max, Hq), torch.float32, dev)
-    if out.data_ptr() == q.data_ptr() and q.numel():   # (workgroups that share a unit read its queries at any time)
+    if abs(out.data_ptr() - q.data_ptr()) < q.nbytes:   # (of one size; workgroups read other units' queries at any time)
         raise ValueError("out must not be q's memory")
     desc = make_desc(B, Hq, Hkv, D, C_max, S_max, _dtype_code(q), grid_blocks)
     if B > 0:

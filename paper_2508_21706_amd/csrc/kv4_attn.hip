@@ -935,6 +935,12 @@ specmoe_verify_desc sized(const specmoe_verify_desc* d) {
   return x;
 }
 
+// [a, a + a_bytes) and [b, b + b_bytes) share memory
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y ? y - x < a_bytes : x - y < b_bytes;
+}
+
 template <int ELT, int D, int PAGING>
 void launch_kv4(const Kv4Params& p, hipStream_t stream) {
   constexpr int kElt = ELT == kF32 ? 4 : 2;
@@ -1014,6 +1020,12 @@ int specmoe_verify_attn_kv4(const void* q, const specmoe_kv4* cache, const int32
                    block_table, paged, p, pl);
   if (st != SPECMOE_OK) return st;
   if (!aligned16(cache->k_scales) || !aligned16(cache->v_scales)) return SPECMOE_ERR_ALIGN;
+  // (workgroups read the queries of some units while others store results)
+  const size_t rows = (size_t)desc->B * desc->C_max * desc->Hq;
+  const size_t row_bytes = (size_t)desc->D * (desc->dtype == SPECMOE_F32 ? 4 : 2);
+  if (overlap(q, rows * row_bytes, out, rows * row_bytes) || overlap(q, rows * row_bytes, lse, rows * sizeof(float)) ||
+      overlap(out, rows * row_bytes, lse, rows * sizeof(float)))
+    return SPECMOE_ERR_OVERLAP;
   if (!paged) p.block_table = nullptr;
   p.k_scales = static_cast<const char*>(cache->k_scales);
   p.v_scales = static_cast<const char*>(cache->v_scales);

@@ -144,6 +144,7 @@ const char* specmoe_status_str(int status) {
     case SPECMOE_ERR_MASK: return "draft masks hold at most 64 draft tokens: C_max must be <= 64";
     case SPECMOE_ERR_HANDOFF: return "an in-kernel wait for another wave gave up: results of a call are unspecified";
     case SPECMOE_ERR_ROPE: return "rot_dim must be a multiple of 16 in [0, D], rope_style and norm_eps valid";
+    case SPECMOE_ERR_OVERLAP: return "out, lse and q must not share memory";
     case SPECMOE_ERR_SCORE: return "softcap and scale / softcap must be finite, softcap and window not negative";
     case SPECMOE_ERR_PAGES:
       return "page_size must be a power of two in [8, 65536], pages_per_seq and num_pages positive, "
