@@ -18,7 +18,10 @@
  * x is written with the smallest unit u >= 2^-126 at which max |x| / u < 7, so
  * that its largest entry rounds to at most 6 and nothing saturates; every code
  * is x / u to the nearest value, ties to the even code.  A block that holds an
- * infinity or NaN becomes a NaN block.
+ * infinity or NaN becomes a NaN block.  Codes of 4 and 6 units with byte 253, and
+ * of 2 and more with 254, stand for values from 2^128 on, past the range of
+ * float32 and bfloat16: they are infinities wherever values are taken in a type.
+ * Of finite entries only those from 1.75 2^127 on come to that (4 units of 2^126).
  *
  * Status codes are the SPECMOE_* values of specmoe_verify.h.  All functions
  * are plain C; pointers named "device" are HIP device pointers.
@@ -132,7 +135,8 @@ typedef struct specmoe_kv4_desc {
  * For every sequence b and i < n_b, the rows f_b + i of its KV heads go to
  * k_out[b, i] and v_out[b, i]: a prefix for a cache of 16 bits, a prompt's rows
  * for its own attention, a request for another machine.  Values are exact in
- * float32 and bfloat16, rounded once (to nearest even) in float16.
+ * float32 and bfloat16, rounded once (to nearest even) in float16; those past the
+ * type's range are infinities.
  *
  *   first        int32 [B], device: f_b (clamped to >= 0).
  *   rows         int32 [B], device: n_b (clamped into [0, N_max]).

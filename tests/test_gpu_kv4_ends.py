@@ -135,6 +135,31 @@ def test_large_finite_entries_appended(dtype):
     assert torch.equal(out[0, 2:, :, 32:], ref[0, 2:, :, 32:])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_values_past_the_types_are_read_as_infinities(dtype):
+    """Every code with the last units: exact in bfloat16 and float32 up to 3 2^126, and
+    infinities with their signs from 2^128 on (in float16 from 65520 on)."""
+    d = dev()
+    codes = torch.from_numpy(np.concatenate([EVERY_CODE] * 2)[None, None, None].repeat(6, 2)).to(d)
+    scales = torch.tensor([[252, 253], [254, 255], [1, 0], [142, 143], [144, 103], [102, 101]],
+                          dtype=torch.uint8, device=d)[None, None]
+    cache = pkg.KV4Cache(codes, scales, codes.clone(), scales.flip(2).contiguous())
+    one = torch.tensor([0], dtype=torch.int32, device=d)
+    k, v = pkg.read_kv4(cache, one, one + 6, 6, dtype=TYPES[dtype])
+    torch.cuda.synchronize()
+    for got, of in ((k, scales), (v, scales.flip(2))):
+        want = decode_ref(codes.cpu().numpy()[0, 0], of.cpu().numpy()[0, 0])
+        bound = {"bf16": 2.0 ** 128, "f32": 2.0 ** 128, "f16": 65520.0}[dtype]
+        got = f64(got)[0, :, 0]
+        for g, w in zip(got.reshape(-1), want.reshape(-1)):
+            if np.isnan(w):
+                assert np.isnan(g)
+            elif abs(w) >= bound:
+                assert g == np.copysign(np.inf, w)
+            else:   # (half a step of float16, 2^-25 of its subnormal ones)
+                assert g == w or dtype == "f16" and abs(g - w) <= max(2.0 ** -11 * abs(w), 2.0 ** -25)
+
+
 TYPES_DIMS = [("bf16", 64), ("bf16", 128), ("f16", 64), ("f16", 128), ("f32", 64), ("f32", 128)]
 
 
