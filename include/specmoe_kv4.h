@@ -16,7 +16,7 @@
  *
  * (The element and scale types of the OCP Microscaling format MXFP4.)  A block
  * x is written with the smallest unit u >= 2^-126 at which max |x| / u < 7, so
- * that its largest entry rounds to at most 6 and nothing saturates; every code
+ * that its largest entry rounds to at most 6 units, none cut down to it; every code
  * is x / u to the nearest value, ties to the even code.  A block that holds an
  * infinity or NaN becomes a NaN block.  Codes of 4 and 6 units with byte 253, and
  * of 2 and more with 254, stand for values from 2^128 on, past the range of

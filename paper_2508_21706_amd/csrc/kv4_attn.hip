@@ -52,6 +52,7 @@ constexpr int kManyTiles = 6, kUnitCost = 4, kSnap = 3;
 // multiple of sqrt(n), and twice that is near it (one sequence of 2,200 keys, 128 rows:
 // 18 pieces 39 us, 8 pieces 33; 13 of 3,700, one KV head, chunks of 3 to 14, float16: 70
 // and 65; 7 of 7,000, 4 KV heads, 126 rows, where 15 pieces leave a few CUs idle: 104, 111).
+// The first rule was measured up to 30,000 keys; past that its units stay at 32 pieces.
 constexpr int kMostPieces = 32;
 constexpr float kPiecesOfRoot = 2.f;
 
@@ -965,7 +966,9 @@ void launch_kv4(const Kv4Params& p, hipStream_t stream) {
     // Row blocks of 16: two to a wave (the conversion of its keys and values serves
     // both: 64 sequences, trees of 16, bf16, four blocks: 63 us; one to a wave 80),
     // but in float32, where two do not fit the registers (8 sequences, chunks of 5,
-    // four heads: 47 us; one to a wave 18).
+    // four heads: 47 us; one to a wave 18): four waves hold up to 64 of its rows, and
+    // more take two all the same, with 110 to 164 registers spilled at D = 128.  (float16
+    // spills 6 to 10 there.)
     const int blocks = (p.Rcap + kBlk - 1) / kBlk;
     const bool single = blocks == 1 || (ELT == kF32 && blocks <= 4);
     if (single) hipLaunchKernelGGL((kv4_attn_kernel<ELT, D, PAGING, 1>), dim3(p.P), dim3(kGroupThreads), 0, stream, s);
